@@ -288,6 +288,113 @@ int32_t knnssd_read_kv(knnssd_ctx *ctx, int32_t block, int32_t pos, float *k_hos
  * current domain outside [0, n_domains), a mix ratio outside [0, 1] or a draw outside [0, 1). */
 int32_t knnssd_stream_next_domain(int32_t current, int32_t n_domains, double mix_ratio, double u_switch, double u_pick);
 
+/* ---- Batches of requests over a paged cache --------------------------------------------------------------------
+ * For callers that take several requests through a model at a time: their own program runs the matrix products, these
+ * calls do what depends on which row belongs to which request. None of them needs a context, allocates memory or waits
+ * for the GPU: everything is put on hip_stream (a stream of the CURRENT device) and may be captured into a HIP graph; the lengths
+ * and tables are read on the device when the work runs, so that a replay follows what has been written there since. Arguments
+ * are checked before anything is launched. What only the device knows is bounded there: a page id outside the cache, a
+ * length beyond the table or a row beyond the batch gives wrong values in the rows concerned, never an access out of range.
+ *
+ * A batch is n_requests requests of which request r has cached[r] positions in the cache and added[r] new rows (tokens: a prompt, a
+ * chunk of one, one token, or drafts to verify; 0 is allowed). The rows of all requests lie one behind the other:
+ * request r's are row_start[r] .. row_start[r+1]-1, at positions cached[r], cached[r]+1, ... Rows behind the last
+ * request's, if a buffer has any, are left as they were.
+ *
+ * One round of a batch: knnssd_page_plan (once), then for every block knnssd_paged_store and knnssd_paged_attention. Calls that
+ * share tables, pages or a workspace have to be ordered (one stream, or events).                                       */
+#define KNNSSD_MAX_REQUESTS 4096
+
+/* The keys and values of one block in pages. Position p of page g and kv head h begins at element
+ * g*page_stride + h*head_stride + p*pos_stride of k_dev and of v_dev: [page][head][position][head_dim] and
+ * [page][position][head][head_dim] are both such orders. Both bases and every stride times the element size are multiples of 16 bytes
+ * (KNNSSD_EINVAL), strides are positive, pos_stride and head_stride at least head_dim. page_size is a power of two from 8 to 1024,
+ * head_dim 64 or 128, n_pages * page_size at most 2^31 - 1 (KNNSSD_ESHAPE). */
+typedef struct knnssd_pages {
+    void *k_dev, *v_dev;
+    int64_t page_stride, head_stride, pos_stride;       /* in elements */
+    int32_t n_pages, page_size, n_kv_heads, head_dim, kv_dtype;
+} knnssd_pages;
+
+/* Which pages belong to whom, on the device. Request r holds the pages block_table[r][0 .. held[r]-1] for its positions
+ * 0 .. held[r]*page_size-1; free_pages[0 .. *n_free-1] is a stack of the pages nobody holds (entries beyond are not looked at). A fresh
+ * pool: held all 0, free_pages any permutation of the page ids, *n_free = n_pages. */
+typedef struct knnssd_page_tables {
+    int32_t *block_table_dev;   /* [n_requests][table_width] */
+    int32_t *held_dev;          /* [n_requests] */
+    int32_t *free_pages_dev;    /* [n_pages] */
+    int32_t *n_free_dev;        /* [1] */
+    int32_t n_requests, table_width, n_pages, page_size;
+} knnssd_page_tables;
+
+/* What the rows of one round are, on the device; all written by knnssd_page_plan. */
+typedef struct knnssd_batch_rows {
+    int32_t *row_start_dev;     /* [n_requests + 1] */
+    int32_t *kv_len_dev;        /* [n_requests] cached + added */
+    int32_t *slots_dev;         /* [max_rows] page * page_size + position in the page; -1 behind the last row */
+    int32_t *positions_dev;     /* [max_rows] position in the request; -1 behind the last row */
+    int32_t *result_dev;        /* [4] rows, pages taken minus pages given back, 0 or what was wrong (below), the longest kv_len */
+    int32_t max_rows;
+} knnssd_batch_rows;
+
+/* Block tables and slots from the requests' lengths. Afterwards request r holds exactly ceil((cached[r] + added[r]) / page_size)
+ * pages: those it no longer needs (rejected drafts, a finished request with cached = added = 0) go back to the stack and their
+ * table entries become -1, then those it lacks are taken. The order is fixed: pages go back in descending order of request
+ * and page and are taken in ascending order, so the same state and lengths give the same tables.
+ * result_dev[2] says in stream order whether it could be done: KNNSSD_PLAN_OK, or one of the following, the first that holds, and then tables and
+ * stack are as they were, row_start and kv_len all 0, slots and positions all -1: the rest of the round does nothing.
+ * KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS] or max_rows < 1, KNNSSD_ESHAPE for a page size or pool outside what knnssd_pages
+ * allows or table_width < 1 or n_requests * table_width > 2^31 - 1. */
+#define KNNSSD_PLAN_OK 0
+#define KNNSSD_PLAN_MALFORMED 1     /* a negative length, or held / n_free outside what the tables can hold */
+#define KNNSSD_PLAN_ROWS 2          /* more than max_rows rows */
+#define KNNSSD_PLAN_WIDTH 3         /* a request needs more than table_width pages */
+#define KNNSSD_PLAN_PAGES 4         /* the pool has too few pages */
+int32_t knnssd_page_plan(const knnssd_page_tables *tables, const int32_t *cached_dev, const int32_t *added_dev,
+                         const knnssd_batch_rows *rows, void *hip_stream);
+
+/* Rotary embedding of a block's queries and keys, and its keys and values into the pages. qkv_dev: [n_rows] rows, qkv_stride elements
+ * apart, of n_heads query heads, then the keys of the kv heads, then their values, head_dim values each (the rows of wqkv), in dtype. Pairs
+ * (i, i + head_dim/2) are turned by position * rope_base^(-2i/head_dim): angles in 64 bits, products in fp32, one
+ * rounding to what is stored. Rotated queries go to q_out_dev (NULL: nowhere), rotated keys also to k_out_dev (NULL: only into the pages),
+ * both in dtype, rows q_out_stride / k_out_stride elements apart; either may lie over the same heads of qkv_dev. Keys and values go to
+ * page slot / page_size, position slot % page_size, in the cache's type. A row whose slot is negative or outside the cache, or whose position is
+ * negative, is skipped: nothing is written for it. No two rows may have the same slot. dtype KNNSSD_BF16 over an fp32 cache is refused
+ * (KNNSSD_EINVAL). n_heads may be 0 (KNNSSD_ERANGE if negative or n_rows < 1). Bases and strides as in knnssd_pages. */
+int32_t knnssd_paged_store(const knnssd_pages *pages, const void *qkv_dev, int32_t dtype, int64_t qkv_stride, int32_t n_rows,
+                           int32_t n_heads, const int32_t *slots_dev, const int32_t *positions_dev, float rope_base,
+                           void *q_out_dev, int64_t q_out_stride, void *k_out_dev, int64_t k_out_stride, void *hip_stream);
+
+/* Attention of the batch's new rows over the pages: row i of request r (n rows, length L = kv_len[r]) attends to positions
+ * 0 .. L - n + i (none: its output is 0), with softmax(scale * q.k); query head h reads kv head h / (n_heads / n_kv_heads). q_dev, out_dev:
+ * [n_rows] rows of n_heads * head_dim values in dtype, q_stride / out_stride elements apart; they must not overlap. dtype is
+ * the cache's type, or KNNSSD_FP32 over a bf16 cache. Scores, softmax and sums are fp32; with dtype KNNSSD_BF16 the weights are rounded to
+ * bf16 for the product with the values. Positions from kv_len on are not looked at; keys and values that a row does not see but a
+ * later one of its request does have to be finite. block_table_dev: [n_requests][table_width]. most_rows: an upper bound of a request's rows
+ * if the caller has one, else 0; it only chooses the kernels. How the sums over a row are grouped follows the batch; the same call gives the
+ * same bits. ws_dev: knnssd_paged_attention_bytes of the same pages, n_heads and dtype (0: not a supported shape), 256-byte aligned, ZEROED
+ * ONCE before its first use; each call leaves it so that the next call, of whatever batch and shape that it is large enough for, can use it.
+ * KNNSSD_ESHAPE where n_heads is not a multiple of n_kv_heads, KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows < 1,
+ * table_width < 1 or a scale that is not finite. */
+size_t knnssd_paged_attention_bytes(const knnssd_pages *pages, int32_t n_heads, int32_t dtype);
+int32_t knnssd_paged_attention(const knnssd_pages *pages, const int32_t *block_table_dev, int32_t table_width,
+                               const int32_t *row_start_dev, const int32_t *kv_len_dev, int32_t n_requests,
+                               const void *q_dev, int64_t q_stride, void *out_dev, int64_t out_stride, int32_t dtype, int32_t n_rows,
+                               int32_t n_heads, float scale, int32_t most_rows, void *ws_dev, size_t ws_bytes, void *hip_stream);
+
+/* Attention of whole prompts, each over itself, causal: rows row_start[r] .. row_start[r+1]-1 are request r's positions 0, 1, ... q, k, v and
+ * out are rows of n_heads (q, out) or n_kv_heads (k, v) heads of head_dim values in dtype, their strides in elements; q, k and v may be parts of
+ * the same rows. Otherwise as knnssd_paged_attention; no pages, no workspace. */
+int32_t knnssd_prompt_attention(const void *q_dev, int64_t q_stride, const void *k_dev, int64_t k_stride, const void *v_dev,
+                                int64_t v_stride, void *out_dev, int64_t out_stride, int32_t dtype, const int32_t *row_start_dev,
+                                int32_t n_requests, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
+                                void *hip_stream);
+
+/* One block of a context's own cache as pages of page_size positions (page g: positions g*page_size ...), so that the calls above read what
+ * knnssd_prefill, knnssd_draft_step and knnssd_verify have written. Host only. KNNSSD_ERANGE for a block outside the model, KNNSSD_ESHAPE if max_seq
+ * is not a multiple of page_size or page_size is not one that knnssd_pages allows. */
+int32_t knnssd_context_pages(const knnssd_ctx *ctx, int32_t block, int32_t page_size, knnssd_pages *pages_out);
+
 /* Message for an error code; for KNNSSD_EHIP the text of the last HIP error of this thread. */
 const char *knnssd_strerror(int32_t code);
 

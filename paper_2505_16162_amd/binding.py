@@ -26,6 +26,8 @@ EXPORTS = [
     "knnssd_set_anchors", "knnssd_prefill", "knnssd_select_skipset", "knnssd_set_skipset", "knnssd_last_selection", "knnssd_knn_topk", "knnssd_route_static",
     "knnssd_draft_step", "knnssd_verify", "knnssd_generate", "knnssd_profile_pass", "knnssd_get_logits", "knnssd_read_kv",
     "knnssd_set_pass_mode", "knnssd_pass_counts", "knnssd_strerror", "knnssd_stream_next_domain",
+    "knnssd_page_plan", "knnssd_paged_store", "knnssd_paged_attention_bytes", "knnssd_paged_attention", "knnssd_prompt_attention",
+    "knnssd_context_pages",
 ]
 
 
@@ -56,6 +58,22 @@ class Stats(ctypes.Structure):
 
     def as_dict(self) -> Dict[str, int]:
         return {n: int(getattr(self, n)) for n, _ in self._fields_}
+
+
+class PagesStruct(ctypes.Structure):
+    _fields_ = [("k_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("pos_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("kv_dtype", ctypes.c_int32)]
+
+
+class PageTablesStruct(ctypes.Structure):
+    _fields_ = [("block_table_dev", ctypes.c_void_p), ("held_dev", ctypes.c_void_p), ("free_pages_dev", ctypes.c_void_p), ("n_free_dev", ctypes.c_void_p),
+                ("n_requests", ctypes.c_int32), ("table_width", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class BatchRowsStruct(ctypes.Structure):
+    _fields_ = [("row_start_dev", ctypes.c_void_p), ("kv_len_dev", ctypes.c_void_p), ("slots_dev", ctypes.c_void_p), ("positions_dev", ctypes.c_void_p),
+                ("result_dev", ctypes.c_void_p), ("max_rows", ctypes.c_int32)]
 
 
 class KnnSsdError(RuntimeError):
@@ -123,6 +141,19 @@ def load_library() -> ctypes.CDLL:
     lib.knnssd_read_kv.argtypes = [vp, i32, i32, vp, vp]
     lib.knnssd_stream_next_domain.restype = i32
     lib.knnssd_stream_next_domain.argtypes = [i32, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double]
+    i64 = ctypes.c_int64
+    lib.knnssd_page_plan.restype = i32
+    lib.knnssd_page_plan.argtypes = [vp, vp, vp, vp, vp]
+    lib.knnssd_paged_store.restype = i32
+    lib.knnssd_paged_store.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, f32, vp, i64, vp, i64, vp]
+    lib.knnssd_paged_attention_bytes.restype = ctypes.c_size_t
+    lib.knnssd_paged_attention_bytes.argtypes = [vp, i32, i32]
+    lib.knnssd_paged_attention.restype = i32
+    lib.knnssd_paged_attention.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, vp, i64, i32, i32, i32, f32, i32, vp, ctypes.c_size_t, vp]
+    lib.knnssd_prompt_attention.restype = i32
+    lib.knnssd_prompt_attention.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i32, i32, i32, i32, i32, f32, vp]
+    lib.knnssd_context_pages.restype = i32
+    lib.knnssd_context_pages.argtypes = [vp, i32, i32, vp]
     lib.knnssd_strerror.restype = ctypes.c_char_p
     lib.knnssd_strerror.argtypes = [i32]
     _lib = lib
@@ -161,6 +192,194 @@ def knnssd_stream_next_domain(current: int, n_domains: int, mix_ratio: float, u_
     if rc < 0:
         _check(rc)
     return int(rc)
+
+
+# ---- batches of requests over a paged cache -------------------------------------------------------------------------
+_TORCH_CODE = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _dtype_code(t: torch.Tensor, name: str) -> int:
+    code = _TORCH_CODE.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    return code
+
+
+def _ints(t: torch.Tensor, device: torch.device, least: int, name: str) -> int:
+    """Address of a contiguous int32 tensor of at least `least` entries on `device`."""
+    if t.dtype != torch.int32 or t.device != device or not t.is_contiguous() or t.numel() < least:
+        raise ValueError(f"{name} must be a contiguous int32 tensor of at least {least} entries on {device}")
+    return t.data_ptr()
+
+
+def _heads(t: torch.Tensor, device: torch.device, head_dim: int, name: str):
+    """(address, row stride, heads) of [rows][heads][head_dim] whose rows may lie apart and whose heads may not."""
+    if t.dim() != 3 or t.device != device:
+        raise ValueError(f"{name} must be [rows][heads][head_dim] on {device}")
+    rows, heads, dim = t.shape
+    stride = t.stride()
+    if dim != head_dim or stride[2] != 1 or (heads > 1 and stride[1] != dim):
+        raise ValueError(f"{name} must have heads of {head_dim} values side by side")
+    return t.data_ptr(), (stride[0] if rows > 1 else heads * dim), heads
+
+
+def _call(device: torch.device, stream: Optional[torch.cuda.Stream], tensors, fn, *args) -> None:
+    """fn(*args, stream) on the device's current stream or on `stream`, with that device current. The tensors stay with the
+    allocator until what `stream` does with them is done."""
+    current = torch.cuda.current_stream(device)
+    if stream is None:
+        stream = current
+    elif stream != current:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+    if torch.cuda.current_device() == device.index:
+        _check(fn(*args, stream.cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, stream.cuda_stream))
+
+
+class Pages:
+    """One block's keys and values in pages: k and v are [n_pages][n_kv_heads][page_size][head_dim] (float32 or bfloat16), in any order in
+    memory in which head_dim is contiguous (a permuted [n_pages][page_size][n_kv_heads][head_dim] too), the same for both."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.device.type != "cuda":
+            raise ValueError("k and v must be [n_pages][n_kv_heads][page_size][head_dim] of one type on one GPU")
+        n_pages, heads, page, dim = k.shape
+        # the stride of a dimension of one entry is never used: any that fits will do
+        strides = [[dim if n == 1 else t.stride(i) for i, n in enumerate((n_pages, heads, page))] for t in (k, v)]
+        if strides[0] != strides[1] or k.stride(3) != 1 or v.stride(3) != 1:
+            raise ValueError("k and v must lie alike in memory, head_dim contiguous")
+        self.k, self.v, self.device, self.head_dim, self.n_kv_heads = k, v, k.device, dim, heads
+        self.struct = PagesStruct(k.data_ptr(), v.data_ptr(), strides[0][0], strides[0][1], strides[0][2], n_pages, page, heads, dim, _dtype_code(k, "k"))
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda:0") -> "Pages":
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device))
+
+
+class PageTables:
+    """Which pages belong to whom (knnssd_page_tables), over the caller's tensors; PageTables.fresh makes those of an unused pool."""
+
+    def __init__(self, block_table: torch.Tensor, held: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, page_size: int):
+        if block_table.dim() != 2 or block_table.device.type != "cuda":
+            raise ValueError("block_table must be [n_requests][table_width] on a GPU")
+        n, width = block_table.shape
+        dev = block_table.device
+        self.block_table, self.held, self.free_pages, self.n_free, self.device, self.n_requests = block_table, held, free_pages, n_free, dev, n
+        self.struct = PageTablesStruct(_ints(block_table, dev, 0, "block_table"), _ints(held, dev, n, "held"), _ints(free_pages, dev, 1, "free_pages"),
+                                       _ints(n_free, dev, 1, "n_free"), n, width, free_pages.numel(), int(page_size))
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def fresh(cls, n_requests: int, max_len: int, n_pages: int, page_size: int, device="cuda:0") -> "PageTables":
+        width = -(-max_len // page_size)
+        return cls(torch.full((n_requests, width), -1, dtype=torch.int32, device=device), torch.zeros(n_requests, dtype=torch.int32, device=device),
+                   torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device), torch.full((1,), n_pages, dtype=torch.int32, device=device), page_size)
+
+
+class BatchRows:
+    """What the rows of a round are (knnssd_batch_rows): row_start, kv_len, slots, positions, result, all written by knnssd_page_plan."""
+
+    def __init__(self, n_requests: int, max_rows: int, device="cuda"):
+        buf = torch.full((2 * n_requests + 1 + 2 * max_rows + 4,), -1, dtype=torch.int32, device=device)
+        self.row_start, self.kv_len, self.slots, self.positions, self.result = buf.split([n_requests + 1, n_requests, max_rows, max_rows, 4])
+        self.device, self.n_requests = buf.device, n_requests
+        self.struct = BatchRowsStruct(*[t.data_ptr() for t in (self.row_start, self.kv_len, self.slots, self.positions, self.result)], max_rows)
+        self.ref = ctypes.byref(self.struct)
+
+
+def knnssd_page_plan(tables: PageTables, rows: BatchRows, cached: torch.Tensor, added: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Pages, block tables and slots of a round from the requests' lengths (int32 [n_requests] on the GPU). rows.result[2] says whether it
+    could be done (KNNSSD_PLAN_*)."""
+    dev, n = tables.device, tables.n_requests
+    if rows.device != dev or rows.n_requests != n:
+        raise ValueError("rows must be made for as many requests, on the same GPU")
+    _call(dev, stream, (tables.block_table, tables.held, tables.free_pages, tables.n_free, rows.row_start, cached, added), load_library().knnssd_page_plan,
+          tables.ref, _ints(cached, dev, n, "cached"), _ints(added, dev, n, "added"), rows.ref)
+
+
+def knnssd_paged_store(pages: Pages, qkv: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor, rope_base: float = 10000.0,
+                       q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Rotary embedding of the rows' queries and keys; keys and values into their slots. qkv: [rows][(n_heads + 2*n_kv_heads)*head_dim];
+    q_out, k_out: [rows][heads][head_dim] of qkv's type, or None (may be the same heads of qkv)."""
+    dev, dim = pages.device, pages.head_dim
+    if qkv.dim() != 2 or qkv.device != dev or qkv.stride(1) != 1 or qkv.shape[1] % dim:
+        raise ValueError(f"qkv must be [rows][heads * {dim}] on {dev}")
+    n_rows, n_heads = qkv.shape[0], qkv.shape[1] // dim - 2 * pages.n_kv_heads
+    outs = []
+    for t, heads, name in ((q_out, n_heads, "q_out"), (k_out, pages.n_kv_heads, "k_out")):
+        if t is None:
+            outs += [None, 0]
+            continue
+        ptr, stride, got = _heads(t, dev, dim, name)
+        if got != heads or t.shape[0] != n_rows or t.dtype != qkv.dtype:
+            raise ValueError(f"{name} must be [{n_rows}][{heads}][{dim}] of {qkv.dtype}")
+        outs += [ptr, stride]
+    _call(dev, stream, (pages.k, pages.v, qkv, slots, positions, q_out, k_out), load_library().knnssd_paged_store, pages.ref, qkv.data_ptr(),
+          _dtype_code(qkv, "qkv"), qkv.stride(0) if n_rows > 1 else qkv.shape[1], n_rows, n_heads, _ints(slots, dev, n_rows, "slots"),
+          _ints(positions, dev, n_rows, "positions"), float(rope_base), *outs)
+
+
+def paged_attention_workspace(pages: Pages, n_heads: int, dtype: torch.dtype) -> torch.Tensor:
+    """A workspace for knnssd_paged_attention on these pages with n_heads query heads of `dtype` (zeroed once, here)."""
+    code = _TORCH_CODE.get(dtype)
+    size = load_library().knnssd_paged_attention_bytes(pages.ref, int(n_heads), -1 if code is None else code)
+    if size == 0:
+        raise KnnSsdError(-2, "shape not supported")
+    return torch.zeros(size, dtype=torch.uint8, device=pages.device)
+
+
+def knnssd_paged_attention(pages: Pages, block_table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor, q: torch.Tensor, workspace: torch.Tensor,
+                           out: Optional[torch.Tensor] = None, scale: Optional[float] = None, most_rows: int = 0,
+                           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Attention of the batch's new rows, q [rows][n_heads][head_dim], over the pages. scale None: 1 / sqrt(head_dim). Without `out` rows
+    behind the last request's hold whatever was there."""
+    dev, dim = pages.device, pages.head_dim
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    qp, qs, n_heads = _heads(q, dev, dim, "q")
+    op, os_, _ = _heads(out, dev, dim, "out")
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must have the shape and type of q")
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [n_requests][table_width]")
+    if workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {dev}")
+    n, width = block_table.shape
+    _call(dev, stream, (pages.k, pages.v, block_table, row_start, kv_len, q, workspace, out), load_library().knnssd_paged_attention, pages.ref,
+          _ints(block_table, dev, 0, "block_table"), width, _ints(row_start, dev, n + 1, "row_start"), _ints(kv_len, dev, n, "kv_len"), n, qp, qs, op, os_,
+          _dtype_code(q, "q"), q.shape[0], n_heads, dim ** -0.5 if scale is None else float(scale), int(most_rows), workspace.data_ptr(),
+          workspace.numel() * workspace.element_size())
+    return out
+
+
+def knnssd_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, out: Optional[torch.Tensor] = None,
+                            scale: Optional[float] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Causal attention of packed prompts, each over itself: q [rows][n_heads][head_dim], k and v [rows][n_kv_heads][head_dim] (parts of one row too),
+    row_start int32 [n_requests + 1]. Without `out` rows behind the last prompt's hold whatever was there."""
+    dev = q.device
+    if dev.type != "cuda" or q.dim() != 3:
+        raise ValueError("q must be [rows][n_heads][head_dim] on a GPU")
+    dim = q.shape[2]
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    qp, qs, n_heads = _heads(q, dev, dim, "q")
+    kp, ks, n_kv = _heads(k, dev, dim, "k")
+    vp, vs, n_v = _heads(v, dev, dim, "v")
+    op, os_, _ = _heads(out, dev, dim, "out")
+    if out.shape != q.shape or n_v != n_kv or k.shape[0] != q.shape[0] or v.shape[0] != q.shape[0]:
+        raise ValueError("q, k, v and out must have the same rows, k and v the same heads, out those of q")
+    if k.dtype != q.dtype or v.dtype != q.dtype or out.dtype != q.dtype:
+        raise ValueError("q, k, v and out must have one type")
+    n = row_start.numel() - 1
+    _call(dev, stream, (q, k, v, row_start, out), load_library().knnssd_prompt_attention, qp, qs, kp, ks, vp, vs, op, os_, _dtype_code(q, "q"),
+          _ints(row_start, dev, 2, "row_start"), n, q.shape[0], n_heads, n_kv, dim, dim ** -0.5 if scale is None else float(scale))
+    return out
 
 
 class KnnSsd:
@@ -366,3 +585,13 @@ class KnnSsd:
         v = torch.empty(kvd, dtype=torch.float32)
         _check(self.lib.knnssd_read_kv(self.h, int(block), int(pos), k.data_ptr(), v.data_ptr()))
         return k, v
+
+    def knnssd_context_pages(self, block: int, page_size: int) -> Pages:
+        """One block of this context's own cache as pages of page_size positions (page g: positions g*page_size ...), as views; max_seq must be
+        a multiple of page_size."""
+        p = PagesStruct()
+        _check(self.lib.knnssd_context_pages(self.h, int(block), int(page_size), ctypes.byref(p)))
+        dtype = torch.bfloat16 if p.kv_dtype == 1 else torch.float32
+        cache = self.kv.view(dtype)
+        at = [(a - self.kv.data_ptr()) // cache.element_size() for a in (p.k_dev, p.v_dev)]
+        return Pages(*[cache.as_strided((p.n_pages, p.n_kv_heads, p.page_size, p.head_dim), (p.page_stride, p.head_stride, p.pos_stride, 1), o) for o in at])

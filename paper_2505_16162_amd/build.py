@@ -8,30 +8,33 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libknnssd.so")
-SOURCES = ["knnssd.hip"]
+SOURCES = ["knnssd.hip", "knnssd_batch.hip"]     # compiled side by side; the kernels that place their own loads are all in the first
 NO_SPILL_KERNELS = ["gemv_kernel", "gemm_mfma_kernel", "prefill_gemm_kernel", "prefill_thin_kernel", "prefill_attn_kernel"]     # mangled-name fragments of the kernels that must not spill
 
 
 def build_library(verbose: bool = False) -> str:
     """Always compiles (hipcc cross-compiles without a GPU present)."""
-    cmd = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    cmd = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-c",
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            "-Wno-unused-command-line-argument",
-           "-I", os.path.join(HERE, "..", "include"),
-           "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
+           "-I", os.path.join(HERE, "..", "include")]
     # The draft GEMV and the verification GEMM issue streaming loads the compiler does not track (hand-placed waits); a register of such a
     # load must never be spilled or copied while the load is in flight. The resource remarks of the same compile
     # tell whether any kernel spills vector registers: the build fails if one of the kernels named below does.
     cmd += ["-Rpass-analysis=kernel-resource-usage"]
     if verbose:
         print(" ".join(cmd))
-    with ThreadPoolExecutor(1) as pool:          # the assembly text is compiled beside the library
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(len(SOURCES) + 1) as pool:      # the assembly text is compiled beside the objects
         text = pool.submit(assembly_text)
-        proc = subprocess.run(cmd, check=False, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
-    remarks = [ln for ln in proc.stderr.splitlines() if "remark:" in ln]
-    other = [ln for ln in proc.stderr.splitlines() if "remark:" not in ln and "kernel-resource-usage" not in ln]
-    if proc.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + proc.stderr[-4000:])
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        procs = list(pool.map(lambda so: _run(cmd + ["-o", so[1], os.path.join(CSRC, so[0])]), zip(SOURCES, objects)))
+        if all(p.returncode == 0 for p in procs):
+            procs.append(_run(["hipcc", "--offload-arch=gfx950", "-fPIC", "-shared", "-o", LIB] + objects))
+    stderr = "\n".join(p.stderr for p in procs)
+    remarks = [ln for ln in stderr.splitlines() if "remark:" in ln]
+    other = [ln for ln in stderr.splitlines() if "remark:" not in ln and "kernel-resource-usage" not in ln]
+    if any(p.returncode != 0 for p in procs):
+        raise RuntimeError("hipcc failed:\n" + "\n".join(p.stderr for p in procs if p.returncode != 0)[-4000:])
     if verbose and other:
         print("\n".join(other))
     current = None
@@ -52,14 +55,18 @@ def build_library(verbose: bool = False) -> str:
     return LIB
 
 
+def _run(cmd):
+    return subprocess.run(cmd, check=False, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
+
+
 def assembly_text() -> str:
-    """The device code as assembly text (a second compile)."""
+    """The device code of the kernels that place their own loads as assembly text (a second compile)."""
     with tempfile.TemporaryDirectory() as tmp:
         asm = os.path.join(tmp, "knnssd.s")
         cmd = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-S", "--cuda-device-only",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument",
-               "-I", os.path.join(HERE, "..", "include"), "-o", asm] + [os.path.join(CSRC, s) for s in SOURCES]
-        proc = subprocess.run(cmd, check=False, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
+               "-I", os.path.join(HERE, "..", "include"), "-o", asm, os.path.join(CSRC, SOURCES[0])]
+        proc = _run(cmd)
         if proc.returncode != 0:
             raise RuntimeError("hipcc -S failed:\n" + proc.stderr[-4000:])
         return open(asm).read()

@@ -11,6 +11,8 @@
 
 #include "../../include/knnssd.h"
 #include "device_types.h"
+#include "hip_try.h"
+#include "pages_check.h"
 #include "knn_plan.h"
 #include "told_wait.h"
 #include "kernels_generic.h"
@@ -21,22 +23,7 @@
 
 using namespace ks;
 
-static thread_local char g_hip_err[256] = "no HIP error recorded";
-
-#define HIP_TRY(expr)                                                                              \
-    do {                                                                                           \
-        hipError_t e_ = (expr);                                                                    \
-        if (e_ != hipSuccess) {                                                                    \
-            snprintf(g_hip_err, sizeof(g_hip_err), "%s at %s:%d", hipGetErrorString(e_), __FILE__, __LINE__); \
-            return KNNSSD_EHIP;                                                                    \
-        }                                                                                          \
-    } while (0)
-
-#define KS_TRY(expr)                    \
-    do {                                \
-        int32_t rc_ = (expr);           \
-        if (rc_ != KNNSSD_OK) return rc_; \
-    } while (0)
+thread_local char g_hip_err[256] = "no HIP error recorded";
 
 static const size_t KS_MAX_DYN_LDS = 160 * 1024;  // dynamic LDS the tuned kernels may ask for (one workgroup per compute unit)
 
@@ -1634,5 +1621,26 @@ extern "C" int32_t knnssd_read_kv(knnssd_ctx *ctx, int32_t block, int32_t pos, f
             }
         }
     }
+    return KNNSSD_OK;
+}
+
+extern "C" int32_t knnssd_context_pages(const knnssd_ctx *ctx, int32_t block, int32_t page_size, knnssd_pages *pages_out) {
+    if (!ctx || !pages_out) return KNNSSD_EINVAL;
+    const knnssd_model_cfg &g = ctx->cfg;
+    if (block < 0 || block >= g.n_blocks) return KNNSSD_ERANGE;
+    if (!page_size_ok(page_size) || g.max_seq % page_size) return KNNSSD_ESHAPE;
+    const size_t elt = g.kv_dtype == KNNSSD_BF16 ? 2 : 4;
+    knnssd_pages p{};
+    p.k_dev = ctx->kv + (size_t)block * ctx->kv_block_bytes;
+    p.v_dev = (char *)p.k_dev + (size_t)g.n_kv_heads * g.max_seq * g.head_dim * elt;
+    p.page_stride = (int64_t)page_size * g.head_dim;
+    p.head_stride = (int64_t)g.max_seq * g.head_dim;
+    p.pos_stride = g.head_dim;
+    p.n_pages = g.max_seq / page_size;
+    p.page_size = page_size;
+    p.n_kv_heads = g.n_kv_heads;
+    p.head_dim = g.head_dim;
+    p.kv_dtype = g.kv_dtype;
+    *pages_out = p;
     return KNNSSD_OK;
 }

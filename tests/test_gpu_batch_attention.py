@@ -1,0 +1,193 @@
+"""Attention over pages and over packed prompts against the definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import batch_common as B
+from paper_2505_16162_amd import binding
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+TYPES = [(BF16, BF16), (F32, BF16), (F32, F32)]
+IDS = ["bf16", "fp32_bf16", "fp32"]
+
+
+def run_paged(c, ws=None, scale=None, most_rows=0, **kw):
+    pages = binding.Pages(c.k_pages, c.v_pages)
+    ws = binding.paged_attention_workspace(pages, c.heads, c.q.dtype) if ws is None else ws
+    return binding.knnssd_paged_attention(pages, c.block_table, c.row_start, c.kv_len, c.q, ws, out=c.out, scale=scale, most_rows=most_rows, **kw)
+
+
+def check_paged(c, scale=None, most_rows=0, ws=None):
+    want, err = c.want(c.dim ** -0.5 if scale is None else scale, BF16 if c.q.dtype == BF16 else None)
+    B.check_rows(run_paged(c, ws, scale, most_rows), want, err, c.q.dtype)
+
+
+FEW = [  # rows, lengths
+    ([1], [1]), ([1], [2]), ([1], [64]), ([1], [65]), ([1], [255]), ([1], [257]), ([2], [1000]), ([1, 0, 3, 1], [5, 0, 3, 40]), ([5, 1, 9, 4, 16], [700, 31, 300, 129, 16]),
+    ([3, 2, 2], [1, 0, 5]),          # rows whose positions lie before the request's first: nothing to see
+    ([0, 0, 2, 0], [100, 0, 70, 9]), ([1] * 40, list(range(1, 200, 5)))]
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 64), (5, 1, 128), (6, 2, 64), (8, 8, 128), (16, 1, 64)])
+@pytest.mark.parametrize("which", range(len(FEW)))
+def test_few_rows(which, heads, kv_heads, dim, types):
+    rows, lens = FEW[which]
+    check_paged(B.PagedCase(rows, lens, heads, kv_heads, dim, 16, *types, seed=which), most_rows=max(rows))
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("page,order", [(8, "head"), (8, "position"), (64, "position"), (256, "head"), (1024, "position")])
+def test_pages_and_orders(page, order, types):
+    check_paged(B.PagedCase([3, 1, 20], [page * 3 + 1, page, page + 19], 6, 3, 128, page, *types, order=order, gap=2), most_rows=20)
+    check_paged(B.PagedCase([2, 70], [9, 2 * page + 71], 4, 2, 64, page, *types, order=order, gap=1))
+
+
+MANY = [([17], [17]), ([33, 1, 65], [33, 90, 300]), ([130], [131]), ([100, 3, 0, 64], [400, 3, 77, 64]), ([200], [199]), ([63, 5], [1, 5])]
+
+
+@pytest.mark.parametrize("hint", [False, True])
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("heads,kv_heads,dim", [(2, 2, 128), (5, 1, 64), (3, 1, 128)])
+@pytest.mark.parametrize("which", range(len(MANY)))
+def test_chunks(which, heads, kv_heads, dim, types, hint):
+    rows, lens = MANY[which]
+    check_paged(B.PagedCase(rows, lens, heads, kv_heads, dim, 32, *types, seed=which), most_rows=max(rows) if hint else 0)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+def test_a_wrong_bound_of_rows_only_costs_time(types):
+    check_paged(B.PagedCase([40, 1], [90, 50], 10, 2, 64, 16, *types), most_rows=1)
+    check_paged(B.PagedCase([1, 1], [90, 50], 10, 2, 64, 16, *types), most_rows=100000)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1.0])
+def test_scales(scale, types):
+    """A scale of 1 makes the softmax nearly one-hot; 0 the mean of the values."""
+    check_paged(B.PagedCase([3, 20], [300, 70], 4, 2, 64, 16, *types), scale=scale)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+def test_scores_far_from_zero(types):
+    """Scores around +-3000 and rising along the axis: the running maximum carries them."""
+    c = B.PagedCase([2, 33], [600, 290], 4, 2, 64, 16, *types)
+    for sign in (1, -1):
+        c.q.fill_(sign * 2.0)
+        for r in range(2):
+            ramp = torch.linspace(100, 187, c.lens[r])[:, None, None].expand_as(c.k[r]).to(c.k[r].dtype)
+            c.k[r] = ramp.contiguous()
+            for j in range(-(-c.lens[r] // 16)):
+                m = min(16, c.lens[r] - j * 16)
+                c.k_pages[c.table[r, j], :, :m] = c.k[r][j * 16:j * 16 + m].permute(1, 0, 2).cuda()
+        check_paged(c, scale=0.125)
+
+
+def test_long_axis_few_rows():
+    """20 000 positions, the last page ending inside a tile; a table of one request of many."""
+    check_paged(B.PagedCase([5, 1], [20011, 37], 5, 1, 128, 64, BF16, BF16), most_rows=5)
+    check_paged(B.PagedCase([2, 1], [9001, 37], 2, 2, 64, 128, F32, BF16), most_rows=2)
+
+
+def test_offsets_beyond_32_bits():
+    """Pages of a pool of more than 2^32 elements: the last ones are read, not their remainders."""
+    n_pages, page, dim = 1, 1024, 128
+    stride = 2 ** 32 // 4 + 8 * 64
+    buf = torch.empty(5 * stride + page * dim, dtype=BF16, device="cuda")
+    k = buf.as_strided((6, 1, page, dim), (stride, page * dim, dim, 1))
+    g = torch.Generator().manual_seed(3)
+    kc, vc = (torch.randn(page, 1, dim, generator=g).to(BF16) for _ in range(2))
+    v = torch.empty_like(buf).as_strided(k.shape, k.stride())
+    k[5, 0], v[5, 0] = kc[:, 0].cuda(), vc[:, 0].cuda()
+    pages = binding.Pages(k, v)
+    for rows, most in ((2, 2), (200, 0)):
+        q = torch.randn(rows, 2, dim, generator=g).to(BF16)
+        out = binding.knnssd_paged_attention(pages, torch.tensor([[5]], dtype=torch.int32, device="cuda"), torch.tensor([0, rows], dtype=torch.int32, device="cuda"),
+                                             torch.tensor([1000], dtype=torch.int32, device="cuda"), q.cuda(), binding.paged_attention_workspace(pages, 2, BF16),
+                                             most_rows=most)
+        want, err = B.attend64(q, kc[:1000], vc[:1000], dim ** -0.5, BF16)
+        B.check_rows(out, want, err, BF16)
+    assert n_pages == 1
+
+
+PROMPTS = [[1], [2, 1], [16], [17, 0, 1], [63, 64, 65], [129, 5], [0, 0, 300, 0], [40] * 7, [255, 257]]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 64), (4, 4, 128), (10, 2, 64), (3, 1, 128)])
+@pytest.mark.parametrize("which", range(len(PROMPTS)))
+def test_prompts(which, heads, kv_heads, dim, dtype):
+    """Packed prompts, queries, keys and values parts of one row; rows behind the last prompt hold NaN and stay out of it."""
+    lens = PROMPTS[which]
+    g = torch.Generator().manual_seed(which)
+    total, pad = sum(lens), 5
+    qkv = torch.randn(total + pad, heads + 2 * kv_heads, dim, generator=g).to(dtype)
+    qkv[total:] = math.nan
+    out = torch.full((total + pad, heads, dim), 5.0, dtype=dtype, device="cuda")
+    start = [0]
+    for a in lens:
+        start.append(start[-1] + a)
+    x = qkv.cuda()
+    q, k, v = x.split([heads, kv_heads, kv_heads], 1)
+    binding.knnssd_prompt_attention(q, k, v, torch.tensor(start, dtype=torch.int32, device="cuda"), out=out)
+    q, k, v = qkv.split([heads, kv_heads, kv_heads], 1)
+    both = [B.attend64(q[a:b], k[a:b], v[a:b], dim ** -0.5, BF16 if dtype == BF16 else None) for a, b in zip(start, start[1:])]
+    B.check_rows(out, torch.cat([o for o, _ in both]), torch.cat([e for _, e in both]), dtype)
+
+
+def test_the_same_call_has_the_same_bits_and_leaves_the_workspace_ready():
+    """One workspace over batches of several shapes, in turn; every repetition has the bits of the first."""
+    cases = [B.PagedCase([2, 1, 5], [900, 3000, 41], 8, 2, 128, 32, BF16, BF16, seed=1), B.PagedCase([1], [5000], 8, 2, 128, 32, BF16, BF16, seed=2),
+             B.PagedCase([70, 1], [800, 700], 8, 2, 128, 32, BF16, BF16, seed=3)]
+    ws = binding.paged_attention_workspace(binding.Pages(cases[0].k_pages, cases[0].v_pages), 8, BF16)
+    first = [run_paged(c, ws).clone() for c in cases]
+    for _ in range(5):
+        for c, f in zip(cases, first):
+            c.out.fill_(5.0)
+            assert torch.equal(run_paged(c, ws), f)
+    for c in cases:
+        check_paged(c, ws=ws)
+
+
+def test_in_a_graph_with_lengths_that_change():
+    """A captured step is replayed with other lengths and tables; eager calls with the same workspace in between."""
+    c = B.PagedCase([4, 3, 1], [2000, 310, 77], 8, 2, 64, 16, BF16, BF16)
+    pages = binding.Pages(c.k_pages, c.v_pages)
+    ws = binding.paged_attention_workspace(pages, 8, BF16)
+    run_paged(c, ws)
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for g in graphs:        # two graphs that share the workspace
+        with torch.cuda.graph(g):
+            run_paged(c, ws)
+    full = list(c.lens)
+    for i, lens in enumerate(([2000, 310, 77], [3, 3, 1], [1999, 1, 0], [700, 300, 60], [2000, 310, 77])):
+        c.lens = lens
+        c.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        c.out.fill_(5.0)
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        got = c.out.clone()
+        keep = c.k, c.v
+        c.k, c.v = [t[:n] for t, n in zip(c.k, lens)], [t[:n] for t, n in zip(c.v, lens)]
+        want, err = c.want(0.125, BF16)
+        B.check_rows(got, want, err, BF16)
+        assert torch.equal(run_paged(c, ws), got)
+        c.k, c.v = keep
+    assert full == c.lens
+
+
+def test_two_streams():
+    """Two batches at once, a workspace each, on streams that are not the tensors' own."""
+    cases = [B.PagedCase([3, 1], [4000, 900], 8, 2, 128, 32, BF16, BF16, seed=s) for s in (1, 2)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    work = [binding.paged_attention_workspace(binding.Pages(c.k_pages, c.v_pages), 8, BF16) for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, s, w in zip(cases, streams, work):
+            run_paged(c, w, stream=s)
+    torch.cuda.synchronize()
+    for c in cases:
+        want, err = c.want(c.dim ** -0.5, BF16)
+        B.check_rows(c.out, want, err, BF16)
