@@ -304,12 +304,13 @@ int32_t knnssd_stream_next_domain(int32_t current, int32_t n_domains, double mix
  * One round of a batch: knnssd_page_plan (once), then for every block knnssd_paged_store and knnssd_paged_attention. Calls that
  * share tables, pages or a workspace have to be ordered (one stream, or events).                                       */
 #define KNNSSD_MAX_REQUESTS 4096
+#define KNNSSD_MAX_ROW_HEADS (1 << 25)      /* rows times query heads of one attention call */
 
 /* The keys and values of one block in pages. Position p of page g and kv head h begins at element
  * g*page_stride + h*head_stride + p*pos_stride of k_dev and of v_dev: [page][head][position][head_dim] and
  * [page][position][head][head_dim] are both such orders. Both bases and every stride times the element size are multiples of 16 bytes
  * (KNNSSD_EINVAL), strides are positive, pos_stride and head_stride at least head_dim. page_size is a power of two from 8 to 1024,
- * head_dim 64 or 128, n_pages * page_size at most 2^31 - 1 (KNNSSD_ESHAPE). */
+ * head_dim 64 or 128, n_pages * page_size at most 2^31 - 1, pos_stride at most 2^26 (KNNSSD_ESHAPE). */
 typedef struct knnssd_pages {
     void *k_dev, *v_dev;
     int64_t page_stride, head_stride, pos_stride;       /* in elements */
@@ -374,8 +375,8 @@ int32_t knnssd_paged_store(const knnssd_pages *pages, const void *qkv_dev, int32
  * if the caller has one, else 0; it only chooses the kernels. How the sums over a row are grouped follows the batch; the same call gives the
  * same bits. ws_dev: knnssd_paged_attention_bytes of the same pages, n_heads and dtype (0: not a supported shape), 256-byte aligned, ZEROED
  * ONCE before its first use; each call leaves it so that the next call, of whatever batch and shape that it is large enough for, can use it.
- * KNNSSD_ESHAPE where n_heads is not a multiple of n_kv_heads, KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows < 1,
- * table_width < 1 or a scale that is not finite. */
+ * KNNSSD_ESHAPE where n_heads is not a multiple of n_kv_heads, KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows < 1 or
+ * n_rows * n_heads > KNNSSD_MAX_ROW_HEADS, table_width < 1 or a scale that is not finite. Lengths beyond 2^30 are taken as 2^30. */
 size_t knnssd_paged_attention_bytes(const knnssd_pages *pages, int32_t n_heads, int32_t dtype);
 int32_t knnssd_paged_attention(const knnssd_pages *pages, const int32_t *block_table_dev, int32_t table_width,
                                const int32_t *row_start_dev, const int32_t *kv_len_dev, int32_t n_requests,
@@ -384,7 +385,7 @@ int32_t knnssd_paged_attention(const knnssd_pages *pages, const int32_t *block_t
 
 /* Attention of whole prompts, each over itself, causal: rows row_start[r] .. row_start[r+1]-1 are request r's positions 0, 1, ... q, k, v and
  * out are rows of n_heads (q, out) or n_kv_heads (k, v) heads of head_dim values in dtype, their strides in elements; q, k and v may be parts of
- * the same rows. Otherwise as knnssd_paged_attention; no pages, no workspace. */
+ * the same rows; k_stride and v_stride at most 2^26 (KNNSSD_ESHAPE). Otherwise as knnssd_paged_attention; no pages, no workspace. */
 int32_t knnssd_prompt_attention(const void *q_dev, int64_t q_stride, const void *k_dev, int64_t k_stride, const void *v_dev,
                                 int64_t v_stride, void *out_dev, int64_t out_stride, int32_t dtype, const int32_t *row_start_dev,
                                 int32_t n_requests, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale,

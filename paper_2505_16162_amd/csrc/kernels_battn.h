@@ -14,6 +14,7 @@ struct BattnArgs {
     int n_requests, n_rows, width, shift, n_pages;
     int H, Hkv, group;
     float scale2;                               // scale * log2(e): softmax in powers of two
+    int few_rows;                               // requests of up to so many rows are another kernel's
 };
 
 // request of row t < row_start[n], by bisection
@@ -25,6 +26,11 @@ __device__ __forceinline__ int battn_request(const int *row_start, int n, int t)
         else hi = mid;
     }
     return lo;
+}
+
+// positions of request r: what its table can hold at most, and no more than 2^30
+__device__ __forceinline__ int battn_len(const BattnArgs &a, int r) {
+    return (int)min((long long)min(max(a.kv_len[r], 0), 1 << 30), (long long)a.width << a.shift);
 }
 
 // element where position p of request r begins for kv head h. A page id outside the cache reads page 0 instead.
@@ -44,7 +50,7 @@ __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
     if (t >= a.n_rows || t >= a.row_start[a.n_requests]) return;
     const int r = battn_request(a.row_start, a.n_requests, t), r0 = max(a.row_start[r], 0);
     const int n = a.row_start[r + 1] - r0;
-    const int len = PAGED ? (int)min((long long)a.kv_len[r], (long long)a.width << a.shift) : n;
+    const int len = PAGED ? battn_len(a, r) : n;
     const int last = PAGED ? min(len - n + (t - r0), len - 1) : t - r0;      // the row's own position
     const int d = (lane % LP) * 8, sub = lane / LP;
     float q[8], o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -85,6 +91,237 @@ __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] *= inv;
         store_values<8>((T *)a.out + t * a.out_stride + h * HD + d, o);
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// Many rows, bf16: tiles of 128 (row, head) pairs of one kv head, 32 per wavefront, on the matrix cores.
+// Everything is computed transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane keeps one pair from the scores to the output: the
+// accumulators of S^T (position 8(i/4) + 4(lane/32) + i%4 of pair lane%32 in register i) are, rounded and packed as they lie, the operand of the
+// second product, whose other operand takes the values' positions in the same order by transposing reads of LDS. Nothing is
+// exchanged between lanes but one maximum per block.
+// Keys and values come in blocks of 64 positions straight to LDS, one block ahead; 16-byte pieces of a row are stored in an order
+// (exclusive or with the row's number) in which neither the keys' reads (32 rows, two pieces each) nor the values' (4 rows, 32
+// bytes each) meet in a bank.
+// ------------------------------------------------------------------------------------------
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+#define BATTN_LDS(p) ((__attribute__((address_space(3))) char *)(p))
+typedef const __attribute__((address_space(4))) int *const_ints;        // read by scalar loads
+
+constexpr int BT_PAIRS = 128, BT_CH = 64;
+
+// 64 lanes' 16 bytes from base + off (bytes) to LDS, lane by lane behind lds_off. Not counted by the compiler: battn_wait. (s_nop: a
+// base that the vector unit has just written may be read five states later.)
+__device__ __forceinline__ void battn_dma(const void *base, unsigned int off, unsigned int lds_off) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(lds_off) : "memory");
+}
+template <int KEEP> __device__ __forceinline__ void battn_wait() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(KEEP) : "memory"); }
+// a workgroup's meeting that leaves loads in flight (this wavefront's LDS reads have returned)
+__device__ __forceinline__ void battn_meet() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+}
+// a * b rounded, also where the compiler could fold the product into a following sum
+__device__ __forceinline__ float battn_rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+
+// Tile `index` of the batch: its request and its number in there; false behind the last. Every wavefront for itself, 64 requests at a time.
+__device__ __forceinline__ bool battn_find_tile(const BattnArgs &a, int index, int &r_out, int &tile_out, int &tiles_out) {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int r0 = 0; r0 < a.n_requests; r0 += 64) {
+        const int r = r0 + lane;
+        int mine = 0;
+        if (r < a.n_requests) {
+            const long long n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
+            if (n > a.few_rows) mine = (int)((n * a.group + BT_PAIRS - 1) / BT_PAIRS);
+        }
+        int upto = mine;
+        for (int off = 1; off < 64; off <<= 1) {
+            const int u = __shfl_up(upto, off);
+            if (lane >= off) upto += u;
+        }
+        const unsigned long long past = __ballot(index < before + upto);
+        if (past) {
+            const int src = __builtin_ctzll(past);
+            r_out = r0 + src;
+            tiles_out = __builtin_amdgcn_readlane(mine, src);
+            tile_out = index - before - (__builtin_amdgcn_readlane(upto, src) - tiles_out);
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+template <int HD> constexpr int battn_tile_lds() { return 2 * 2 * BT_CH * HD * 2; }
+
+template <int HD, bool PAGED>
+__global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
+    constexpr int KS = HD / 16, DT = HD / 32, SL = HD / 8, RB = HD * 2;
+    constexpr int KV = BT_CH * RB;                            // bytes of a block's keys (or values)
+    constexpr int ROWS = 64 / SL, NI = KV / 1024 / 4;         // rows a wavefront's load covers, loads per wavefront for the keys
+    extern __shared__ __align__(16) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int kvh = blockIdx.x % a.Hkv;                       // (a kv head's tiles run behind few L2s)
+    int r, tile, n_tiles;
+    if (!battn_find_tile(a, blockIdx.x / a.Hkv, r, tile, n_tiles)) return;
+    tile = n_tiles - 1 - tile;                                // long ones first
+    const int r0 = max(a.row_start[r], 0), n = min(a.row_start[r + 1], a.n_rows) - r0;
+    const int len = PAGED ? battn_len(a, r) : n;
+    const int base = len - n;                                 // position of the request's first new row
+    const long long pairs = (long long)n * a.group, p0 = (long long)tile * BT_PAIRS;
+    const int wave_first = (int)((p0 + wave * 32) / a.group);                                                  // the wavefront's first row
+    const int wave_last = (int)(min(p0 + wave * 32 + 31, pairs - 1) / a.group);                                  // ... and last one
+    const int tile_last = (int)(min(p0 + BT_PAIRS - 1, pairs - 1) / a.group);
+    const int n_blocks = base + tile_last < 0 ? 0 : (base + tile_last) / BT_CH + 1;
+    const long long pair = p0 + wave * 32 + col;
+    const bool live = pair < pairs;
+    const int row = (int)(min(pair, pairs - 1) / a.group), g = (int)(min(pair, pairs - 1) % a.group);
+    const int limit = base + row;                             // the lane's last visible position
+    const int last = len - 1;
+    const unsigned int l0 = (unsigned int)(uintptr_t)BATTN_LDS(lds);
+    const bf16_t *kb = (const bf16_t *)a.k, *vb = (const bf16_t *)a.v;
+    if constexpr (PAGED) { kb += kvh * a.head_stride; vb += kvh * a.head_stride; }
+    else { kb += (long long)r0 * a.k_stride + kvh * HD; vb += (long long)r0 * a.v_stride + kvh * HD; }
+    const const_ints table = (const_ints)(uintptr_t)(a.table + (PAGED ? (size_t)r * a.width : 0));
+
+    // first row of the wavefront's i-th load of block c (rows past the request's last repeat that one)
+    auto load_row = [&](int c, int i) { return min(c * BT_CH + (i * 4 + wave) * ROWS, last & -ROWS); };
+    const int kpiece = (lane % SL) ^ ((wave * ROWS + lane / SL) & (SL - 1)), vpiece = (lane % SL) ^ (((lane / SL) & 3) << 1);
+    int page[NI];
+    auto look_up = [&](int c) {                               // the pages of block c
+        if constexpr (PAGED)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) page[i] = table[load_row(c, i) >> a.shift];
+    };
+    auto issue = [&](int c, int buf) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int b = load_row(c, i), in = min(lane / SL, last - b);
+            const unsigned int d = l0 + buf * 2 * KV + (i * 4 + wave) * 1024;
+            if constexpr (PAGED) {
+                const int pg = (unsigned)page[i] < (unsigned)a.n_pages ? page[i] : 0;
+                const long long at = pg * a.page_stride + (b & ((1 << a.shift) - 1)) * a.pos_stride;
+                const unsigned int off = (unsigned int)in * (unsigned int)a.pos_stride * 2u;
+                battn_dma(kb + at, off + kpiece * 16, d);
+                battn_dma(vb + at, off + vpiece * 16, d + KV);
+            } else {
+                battn_dma(kb + b * a.k_stride, (unsigned int)in * (unsigned int)a.k_stride * 2u + kpiece * 16, d);
+                battn_dma(vb + b * a.v_stride, (unsigned int)in * (unsigned int)a.v_stride * 2u + vpiece * 16, d + KV);
+            }
+        }
+    };
+    if (n_blocks > 0) {
+        look_up(0);
+        issue(0, 0);
+        look_up(1);
+    }
+    bf16x8_t qf[KS];                                          // dimensions 16 ks + 8 half ... of the lane's pair
+    {
+        const bf16_t *qp = (const bf16_t *)a.q + (long long)(r0 + row) * a.q_stride + (kvh * a.group + g) * HD + half * 8;
+        const unsigned int flip = a.scale2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(qp + ks * 16) ^ flip);
+    }
+    const float c2 = fabsf(a.scale2);
+    float m = -INFINITY, off = -INFINITY, l = 0.f;
+    f32x16_t o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    const int k_at = col * RB, v_row = 4 * half + ((lane & 15) >> 2), v_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+
+    for (int c = 0; c < n_blocks; ++c) {
+        const int buf = c & 1;
+        battn_wait<0>();
+        battn_meet();                                         // block c is here and nobody reads block c-1 any more
+        if (c + 1 < n_blocks) {
+            issue(c + 1, buf ^ 1);
+            look_up(c + 2);
+        }
+        if (c * BT_CH > base + wave_last) continue;           // beyond all of the wavefront's rows
+        const char *kl = lds + buf * 2 * KV;
+        const unsigned int vl = l0 + buf * 2 * KV + KV;
+        f32x16_t s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(kl + t * 32 * RB + k_at + (((2 * ks + half) ^ (col & (SL - 1))) * 16)));
+                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s[t], 0, 0, 0);
+            }
+        }
+        const bool diagonal = c * BT_CH + BT_CH - 1 > base + wave_first;
+        if (diagonal) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (c * BT_CH + t * 32 + 8 * (i / 4) + 4 * half + i % 4 > limit) s[t][i] = -INFINITY;
+        }
+        float cm = s[0][0];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) cm = fmaxf(cm, s[t][i]);
+        cm = fmaxf(cm, lane_xor(cm, 32));
+        m = fmaxf(m, cm);
+        const float off_new = m == -INFINITY ? 0.f : battn_rounded_product(m, c2), f = __builtin_amdgcn_exp2f(off - off_new);
+        off = off_new;
+        float ps = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], c2, -off));
+                if (diagonal && c * BT_CH + t * 32 + 8 * (i / 4) + 4 * half + i % 4 > limit) s[t][i] = 0.f;      // (also where the scale is 0)
+                ps += s[t][i];
+            }
+        l = l * f + ps;
+        if (__any(f != 1.0f)) {
+#pragma unroll
+            for (int t = 0; t < DT; ++t) o[t] *= f;
+        }
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {                      // 16 positions
+            const int t = st >> 1, i0 = (st & 1) * 8;
+            const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16(s[t][i0], s[t][i0 + 1]), pack_bf16(s[t][i0 + 2], s[t][i0 + 3]),
+                                                                     pack_bf16(s[t][i0 + 4], s[t][i0 + 5]), pack_bf16(s[t][i0 + 6], s[t][i0 + 7])});
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                // (rows st*16 + v_row and 8 on: the row's number ends in v_row & 3, whatever st)
+                const unsigned int at = vl + (st * 16 + v_row) * RB + (((4 * dt + (v_col >> 3)) ^ ((v_row & 3) << 1)) * 16) + (v_col & 4) * 2;
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)at);
+                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)(at + 8 * RB));
+                const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb, o[dt], 0, 0, 0);
+            }
+        }
+    }
+    l += lane_xor(l, 32);
+    if (live) {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        bf16_t *op = (bf16_t *)a.out + (long long)(r0 + row) * a.out_stride + (kvh * a.group + g) * HD + 4 * half;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const float v[4] = {o[t][4 * b] * inv, o[t][4 * b + 1] * inv, o[t][4 * b + 2] * inv, o[t][4 * b + 3] * inv};
+                store_values<4>(op + t * 32 + b * 8, v);
+            }
     }
 }
 

@@ -75,12 +75,18 @@ static int32_t rows_check(const int32_t *row_start_dev, int32_t n_requests, cons
     if (!row_start_dev || !q || !out || !dtype_ok(dtype)) return KNNSSD_EINVAL;
     if (n_requests < 1 || n_requests > KNNSSD_MAX_REQUESTS || n_rows < 1 || !std::isfinite(scale)) return KNNSSD_ERANGE;
     if (n_heads < 1 || n_heads > 65535 || n_heads % n_kv_heads) return KNNSSD_ESHAPE;
+    if ((int64_t)n_rows * n_heads > KNNSSD_MAX_ROW_HEADS) return KNNSSD_ERANGE;
     if (!rows_ok(q, q_stride, n_heads * hd, dtype) || !rows_ok(out, out_stride, n_heads * hd, dtype)) return KNNSSD_EINVAL;
     return KNNSSD_OK;
 }
 
 template <int HD, bool PAGED>
 static void launch_battn(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, hipStream_t s) {
+    if (dtype == KNNSSD_BF16) {
+        const int64_t tiles = ((int64_t)a.n_rows * a.group + BT_PAIRS - 1) / BT_PAIRS + a.n_requests;       // (at most; what is too much ends at once)
+        hipLaunchKernelGGL((battn_tile_kernel<HD, PAGED>), dim3((unsigned)(tiles * a.Hkv)), dim3(256), battn_tile_lds<HD>(), s, a);
+        return;
+    }
     const int64_t items = (int64_t)a.n_rows * a.H;
     const dim3 grid((unsigned)((items + 3) / 4));
     if (dtype == KNNSSD_BF16) hipLaunchKernelGGL((battn_row_kernel<HD, PAGED, bf16_t, bf16_t>), grid, dim3(256), 0, s, a);
@@ -125,6 +131,7 @@ extern "C" int32_t knnssd_prompt_attention(const void *q_dev, int64_t q_stride, 
     if ((head_dim != 64 && head_dim != 128) || n_kv_heads < 1) return KNNSSD_ESHAPE;
     KS_TRY(rows_check(row_start_dev, n_requests, q_dev, q_stride, out_dev, out_stride, dtype, n_rows, n_heads, n_kv_heads, head_dim, scale));
     if (!rows_ok(k_dev, k_stride, (int64_t)n_kv_heads * head_dim, dtype) || !rows_ok(v_dev, v_stride, (int64_t)n_kv_heads * head_dim, dtype)) return KNNSSD_EINVAL;
+    if (k_stride > MAX_ROW_STRIDE || v_stride > MAX_ROW_STRIDE) return KNNSSD_ESHAPE;
     BattnArgs a{};
     a.q = q_dev; a.k = k_dev; a.v = v_dev; a.out = out_dev; a.q_stride = q_stride; a.out_stride = out_stride; a.k_stride = k_stride; a.v_stride = v_stride;
     a.row_start = row_start_dev; a.n_requests = n_requests; a.n_rows = n_rows;

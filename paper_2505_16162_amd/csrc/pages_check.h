@@ -12,8 +12,11 @@ static inline int64_t dtype_bytes(int32_t t) { return t == KNNSSD_BF16 ? 2 : 4; 
 
 // rows (or pages) read and written in 16-byte pieces: the base, and a stride of at least `least` elements
 static inline bool rows_ok(const void *base, int64_t stride, int64_t least, int32_t dtype) {
-    return !((uintptr_t)base & 15) && stride >= least && !((stride * dtype_bytes(dtype)) & 15);
+    return !((uintptr_t)base & 15) && stride >= least && stride <= INT64_MAX / 8 && !((stride * dtype_bytes(dtype)) & 15);
 }
+
+// distance of neighbouring positions (or rows of keys), which the kernels count in 32 bits of bytes over a few of them
+static const int64_t MAX_ROW_STRIDE = 1 << 26;
 
 // KNNSSD_OK, or what is wrong with a paged cache
 static inline int32_t pages_check(const knnssd_pages *p) {
@@ -24,7 +27,7 @@ static inline int32_t pages_check(const knnssd_pages *p) {
     if (!rows_ok(p->k_dev, p->pos_stride, p->head_dim, p->kv_dtype) || !rows_ok(p->v_dev, p->head_stride, p->head_dim, p->kv_dtype) ||
         !rows_ok(p->k_dev, p->page_stride, p->head_dim, p->kv_dtype))
         return KNNSSD_EINVAL;
-    return KNNSSD_OK;
+    return p->pos_stride > MAX_ROW_STRIDE ? KNNSSD_ESHAPE : KNNSSD_OK;
 }
 
 // the types that rows and a cache may have together
