@@ -14,7 +14,8 @@ struct BattnArgs {
     int n_requests, n_rows, width, shift, n_pages;
     int H, Hkv, group;
     float scale2;                               // scale * log2(e): softmax in powers of two
-    int few_rows;                               // requests of up to so many rows are another kernel's
+    int few_rows;                               // requests of up to so many rows are battn_few_kernel's
+    void *ws;
 };
 
 // request of row t < row_start[n], by bisection
@@ -39,9 +40,9 @@ __device__ __forceinline__ long long battn_paged(const BattnArgs &a, int r, int 
     return ((unsigned)g < (unsigned)a.n_pages ? g : 0) * a.page_stride + h * a.head_stride + (p & ((1 << a.shift) - 1)) * a.pos_stride;
 }
 
-// A wavefront per (row, head), for any types: the lanes that share a position take eight dimensions each, 64 / (HD / 8) positions at a time;
+// A wavefront per (row, head), fp32: the lanes that share a position take eight dimensions each, 64 / (HD / 8) positions at a time;
 // each such group of lanes keeps its own running maximum and sum, merged at the end.
-template <int HD, bool PAGED, typename T, typename KT>
+template <int HD, bool PAGED>
 __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
     constexpr int LP = HD / 8, NP = 64 / LP;
     const int lane = threadIdx.x & 63;
@@ -54,9 +55,9 @@ __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
     const int last = PAGED ? min(len - n + (t - r0), len - 1) : t - r0;      // the row's own position
     const int d = (lane % LP) * 8, sub = lane / LP;
     float q[8], o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const T *qp = (const T *)a.q + t * a.q_stride + h * HD + d;
+    const float *qp = (const float *)a.q + t * a.q_stride + h * HD + d;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[e] = load_as_float(qp, e);
+    for (int e = 0; e < 8; ++e) q[e] = qp[e];
     float m = -INFINITY, l = 0.f;
     for (int p = sub; p <= last; p += NP) {
         long long ko, vo;
@@ -66,17 +67,17 @@ __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
             ko = (long long)(r0 + p) * a.k_stride + kvh * HD;
             vo = (long long)(r0 + p) * a.v_stride + kvh * HD;
         }
-        const KT *kp = (const KT *)a.k + ko + d, *vp = (const KT *)a.v + vo + d;
+        const float *kp = (const float *)a.k + ko + d, *vp = (const float *)a.v + vo + d;
         float s = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s = fmaf(q[e], load_as_float(kp, e), s);
+        for (int e = 0; e < 8; ++e) s = fmaf(q[e], kp[e], s);
         for (int off = 1; off < LP; off <<= 1) s += __shfl_xor(s, off);
         s *= a.scale2;
         const float mn = fmaxf(m, s), f = exp2f(m - mn), w = exp2f(s - mn);
         l = l * f + w;
         m = mn;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = fmaf(w, load_as_float(vp, e), o[e] * f);
+        for (int e = 0; e < 8; ++e) o[e] = fmaf(w, vp[e], o[e] * f);
     }
     for (int off = LP; off < 64; off <<= 1) {
         const float m2 = __shfl_xor(m, off), l2 = __shfl_xor(l, off), mn = fmaxf(m, m2);
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
         const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] *= inv;
-        store_values<8>((T *)a.out + t * a.out_stride + h * HD + d, o);
+        store_values<8>((float *)a.out + t * a.out_stride + h * HD + d, o);
     }
 }
 
@@ -322,6 +323,370 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
                 const float v[4] = {o[t][4 * b] * inv, o[t][4 * b + 1] * inv, o[t][4 * b + 2] * inv, o[t][4 * b + 3] * inv};
                 store_values<4>(op + t * 32 + b * 8, v);
             }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// Few rows over a bf16 cache: what bounds them is the cache, read once. A request's (row, head) pairs of one kv head, 16 NT at a time, against
+// all of its positions are a group; a group's blocks of 64 (32 where more pairs share them) positions are units, and the units of the whole batch, group behind
+// group, are dealt to the workgroups in equal runs (worked out by each for itself from the lengths). The four wavefronts of a workgroup take the
+// blocks of a run in turn, keys and values straight from the cache to registers as operands, and are merged in LDS where a group ends. A
+// group that lies in several runs leaves a partial result per run in the workspace, and the workgroup that counts itself in last merges them,
+// in the order of the runs. Nobody waits for anybody; the counter goes back to zero.
+// As in the tile kernel everything is transposed, here in 16 x 16 tiles. Values are regrouped by byte permutes: a lane takes HD/16 neighbouring
+// dimensions of its eight positions, so that matrix instruction t yields dimensions {HD/16 n + t}.
+// NP = 3: fp32 queries, which stay exact as three bf16 planes, as do the weights.
+// ------------------------------------------------------------------------------------------
+constexpr int BF_WGS = 512;                                   // two workgroups per compute unit: 256 KB of the cache in flight on each
+constexpr int BF_PAD = 4;                                     // floats behind a pair's HD values: its exponent, its sum
+
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+// positions of a unit: what a wavefront holds in registers beside its accumulators
+template <int HD> __host__ __device__ constexpr int battn_few_positions(int nt) { return HD == 128 && nt > 1 ? 32 : 64; }
+template <int HD> __host__ __device__ constexpr size_t battn_few_slot(int pairs) { return (size_t)pairs * (HD + BF_PAD); }      // floats of a partial result
+__host__ __device__ constexpr size_t battn_few_counters() { return BF_WGS * sizeof(int); }
+
+// eight fp32 values as NP bf16 operands: rounded to nearest (1), or cut three times into exact parts (3)
+template <int NP>
+__device__ __forceinline__ void battn_planes(const float *v, bf16x8_t *out) {
+    if constexpr (NP == 1) {
+        out[0] = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])});
+    } else {
+        float rest[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rest[e] = v[e];
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            u32x4_t w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[e] = __builtin_amdgcn_perm(__float_as_uint(rest[2 * e + 1]), __float_as_uint(rest[2 * e]), 0x07060302u);
+                rest[2 * e] -= __uint_as_float(w[e] << 16);
+                rest[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+            }
+            out[p] = __builtin_bit_cast(bf16x8_t, w);
+        }
+    }
+}
+
+// units of request r: rows (0: not this kernel's), blocks of a group, groups of pairs per kv head
+struct FewShape { int n, blocks, pair_groups; };
+__device__ __forceinline__ FewShape battn_few_shape(const BattnArgs &a, int r, int group_pairs, int positions) {
+    FewShape f{0, 1, 0};
+    const int n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
+    if (n > 0 && n <= a.few_rows) {
+        f.n = n;
+        f.blocks = max(1, (battn_len(a, r) + positions - 1) / positions);
+        f.pair_groups = (int)(((long long)n * a.group + group_pairs - 1) / group_pairs);
+    }
+    return f;
+}
+
+template <int HD, int NT, int PW, int NP>
+__host__ __device__ constexpr int battn_few_lds() {
+    // the queries of a group [plane][pair][HD + 8] in bf16, and the wavefronts' shares [4][16][HD + BF_PAD] of one tile
+    return NP * PW * NT * 16 * (HD + 8) * 2 + 4 * 16 * (HD + BF_PAD) * 4;
+}
+
+// V values of one pair, divided by the sum of its weights
+template <int V, int HD, int NP>
+__device__ __forceinline__ void battn_few_out(const BattnArgs &a, int r0, int kvh, int pair, int d, float *v, float sum) {
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] *= inv;
+    const long long at = (long long)(r0 + pair / a.group) * a.out_stride + (kvh * a.group + pair % a.group) * HD + d;
+    if constexpr (NP == 1) store_values<V>((bf16_t *)a.out + at, v);
+    else store_values<V>((float *)a.out + at, v);
+}
+
+template <int HD, int NT, int PW, int NP>
+__global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
+    constexpr int QS = HD / 32, DT = HD / 16, QROW = HD + 8, MROW = HD + BF_PAD, PAIRS = 16 * NT * PW, CH = battn_few_positions<HD>(NT), PT = CH / 16;
+    typedef unsigned int vword __attribute__((ext_vector_type(DT / 2)));
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int ticket;
+    bf16_t *ql = (bf16_t *)lds;
+    float *mb = (float *)(lds + NP * PAIRS * QROW * 2);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kg = lane >> 4, n16 = lane & 15;
+    const int wp = wave % PW, wb = wave / PW, wave_pair = wp * 16 * NT;      // the wavefront's pairs, its blocks: wb, wb + 4/PW, ...
+    float *slots = (float *)((char *)a.ws + battn_few_counters());
+    int *counters = (int *)a.ws;
+
+    // all units, and the first of this workgroup's run: how many requests lie before it, their units
+    long long total = 0;
+    for (int r0 = 0; r0 < a.n_requests; r0 += 64) {
+        const int r = r0 + lane;
+        long long mine = 0;
+        if (r < a.n_requests) {
+            const FewShape f = battn_few_shape(a, r, PAIRS, CH);
+            mine = (long long)f.blocks * f.pair_groups * a.Hkv;
+        }
+        for (int off = 32; off; off >>= 1) mine += __shfl_xor(mine, off);
+        total += mine;
+    }
+    const int runs = (int)min((long long)gridDim.x, (total + 3) / 4);           // four units at least: a block for every wavefront
+    const int w = blockIdx.x;
+    if (w >= runs) return;
+    auto run_start = [&](int i) { return (long long)i * total / runs; };
+    auto run_of = [&](long long unit) { return (int)(((unit + 1) * runs - 1) / total); };
+    long long unit = run_start(w);
+    const long long unit_end = run_start(w + 1);
+    long long before = 0;                                     // units before request r
+    int r = 0;
+    FewShape f{0, 1, 0};
+    {
+        for (int r0 = 0; r0 < a.n_requests; r0 += 64) {
+            long long upto = 0;
+            if (r0 + lane < a.n_requests) {
+                const FewShape g = battn_few_shape(a, r0 + lane, PAIRS, CH);
+                upto = (long long)g.blocks * g.pair_groups * a.Hkv;
+            }
+            for (int off = 1; off < 64; off <<= 1) {
+                const long long u = __shfl_up(upto, off);
+                if (lane >= off) upto += u;
+            }
+            const unsigned long long past = __ballot(unit < before + upto);
+            if (past) {
+                const int src = __builtin_ctzll(past);
+                r = r0 + src;
+                if (src > 0) before += __shfl(upto, src - 1);
+                break;
+            }
+            before += __shfl(upto, 63);
+        }
+        r = __builtin_amdgcn_readfirstlane(r);
+        f = battn_few_shape(a, r, PAIRS, CH);
+    }
+    const float c2 = fabsf(a.scale2);
+    const unsigned int flip = a.scale2 < 0.f ? 0x80000000u : 0u;
+
+    while (unit < unit_end) {
+        while (unit - before >= (long long)f.blocks * f.pair_groups * a.Hkv) {   // on to the next request with units
+            before += (long long)f.blocks * f.pair_groups * a.Hkv;
+            if (++r >= a.n_requests) return;                  // (never: the units lie in some request)
+            f = battn_few_shape(a, r, PAIRS, CH);
+        }
+        const long long in = unit - before;
+        const int group = (int)(in / f.blocks), b0 = (int)(in - (long long)group * f.blocks);
+        const int kvh = group / f.pair_groups, pg = group - kvh * f.pair_groups;
+        const int b1 = (int)min((long long)f.blocks, b0 + (unit_end - unit));
+        const int r0 = max(a.row_start[r], 0), n = f.n, len = battn_len(a, r), base = len - n, last = len - 1;
+        const int pairs = min(PAIRS, n * a.group - pg * PAIRS);                  // (n * group: at most the rows and heads of a call)
+
+        // the group's queries
+        __syncthreads();
+        for (int i = tid; i < PAIRS * (HD / 8); i += 256) {
+            const int p = i / (HD / 8), d = (i % (HD / 8)) * 8, pair = pg * PAIRS + min(p, pairs - 1);
+            const long long at = (long long)(r0 + pair / a.group) * a.q_stride + (kvh * a.group + pair % a.group) * HD + d;
+            if constexpr (NP == 1) {
+                *reinterpret_cast<u32x4_t *>(ql + p * QROW + d) = *reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + at) ^ (flip | flip >> 16);
+            } else {
+                float v[8];
+                bf16x8_t planes[3];
+                Piece<float>::load((const float *)a.q + at, v);
+                Piece<float>::load((const float *)a.q + at + 4, v + 4);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(__float_as_uint(v[e]) ^ flip);
+                battn_planes<3>(v, planes);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<bf16x8_t *>(ql + (q * PAIRS + p) * QROW + d) = planes[q];
+            }
+        }
+        __syncthreads();
+
+        int limit[NT];                                        // a pair's last visible position
+        float off[NT], l[NT];
+        f32x4_t o[NT][DT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            limit[t] = base + (pg * PAIRS + min(wave_pair + t * 16 + n16, pairs - 1)) / a.group;
+            off[t] = -INFINITY;
+            l[t] = 0.f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        const int first_limit = base + pg * PAIRS / a.group;
+        const const_ints table = (const_ints)(uintptr_t)(a.table + (size_t)r * a.width);
+        const bf16_t *kb = (const bf16_t *)a.k + kvh * a.head_stride, *vb = (const bf16_t *)a.v + kvh * a.head_stride;
+        if (len > 0) {
+            for (int b = b0 + wb; b < b1 && wave_pair < pairs; b += 4 / PW) {
+                const int pos0 = b * CH;
+                u32x4_t kf[PT][QS];                            // position 16 pt + n16, dimensions 32 ks + 8 kg ...
+                vword vr[PT][4];                               // position 16 pt + 4 kg + i, dimensions DT n16 ...
+#pragma unroll
+                for (int pt = 0; pt < PT; ++pt) {
+                    // the tile's positions eight by eight: a page holds at least so many. Positions past the last one repeat it.
+                    long long at[2];
+                    int in8[2], rest[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int p = min(pos0 + pt * 16 + e * 8, last & -8), id = table[p >> a.shift];
+                        at[e] = ((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.page_stride + (p & ((1 << a.shift) - 1)) * a.pos_stride;
+                        rest[e] = last - p;
+                    }
+                    in8[0] = min(n16 & 7, n16 & 8 ? rest[1] : rest[0]);
+                    const bf16_t *kp = kb + (n16 & 8 ? at[1] : at[0]) + in8[0] * a.pos_stride + kg * 8;
+#pragma unroll
+                    for (int ks = 0; ks < QS; ++ks) kf[pt][ks] = *reinterpret_cast<const u32x4_t *>(kp + ks * 32);
+                    const bf16_t *vp = vb + (kg & 2 ? at[1] : at[0]) + n16 * DT;
+                    const int vrest = kg & 2 ? rest[1] : rest[0];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) vr[pt][i] = *reinterpret_cast<const vword *>(vp + min((kg & 1) * 4 + i, vrest) * a.pos_stride);
+                }
+                __builtin_amdgcn_sched_barrier(0);            // every load is on its way before the first is waited for
+                const bool diagonal = pos0 + CH - 1 > first_limit;
+                u32x4_t vf[PT / 2][DT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    if (wave_pair + t * 16 >= pairs) break;
+                    f32x4_t s[PT];
+#pragma unroll
+                    for (int pt = 0; pt < PT; ++pt) s[pt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                    // the lowest plane first
+#pragma unroll
+                    for (int q = NP - 1; q >= 0; --q)
+#pragma unroll
+                        for (int ks = 0; ks < QS; ++ks) {
+                            const bf16x8_t qf = *reinterpret_cast<const bf16x8_t *>(ql + (q * PAIRS + wave_pair + t * 16 + n16) * QROW + ks * 32 + kg * 8);
+#pragma unroll
+                            for (int pt = 0; pt < PT; ++pt) s[pt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[pt][ks]), qf, s[pt], 0, 0, 0);
+                        }
+                    if (diagonal) {
+#pragma unroll
+                        for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (pos0 + pt * 16 + 4 * kg + i > limit[t]) s[pt][i] = -INFINITY;
+                    }
+                    float cm = s[0][0];
+#pragma unroll
+                    for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) cm = fmaxf(cm, s[pt][i]);
+                    cm = fmaxf(cm, lane_xor(cm, 16));
+                    cm = fmaxf(cm, lane_xor(cm, 32));
+                    // (-inf times a scale of 0 would be NaN)
+                    const float off_new = cm == -INFINITY ? off[t] : fmaxf(off[t], battn_rounded_product(cm, c2)), ref = off_new == -INFINITY ? 0.f : off_new;
+                    const float fac = __builtin_amdgcn_exp2f(off[t] - ref);
+                    off[t] = off_new;
+                    float ps = 0.f;
+#pragma unroll
+                    for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            s[pt][i] = __builtin_amdgcn_exp2f(fmaf(s[pt][i], c2, -ref));
+                            if (diagonal && pos0 + pt * 16 + 4 * kg + i > limit[t]) s[pt][i] = 0.f;
+                            ps += s[pt][i];
+                        }
+                    l[t] = l[t] * fac + ps;
+                    if (__any(fac != 1.0f)) {
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) o[t][d] *= fac;
+                    }
+                    if (t == 0) {                             // the values' operands, once for all tiles: positions 2j, 2j+1 of the lane's eight
+#pragma unroll
+                        for (int hf = 0; hf < PT / 2; ++hf)
+#pragma unroll
+                            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    vf[hf][d][j] = __builtin_amdgcn_perm(vr[2 * hf + (j >> 1)][2 * (j & 1) + 1][d >> 1], vr[2 * hf + (j >> 1)][2 * (j & 1)][d >> 1],
+                                                                         (d & 1) ? 0x07060302u : 0x05040100u);
+                    }
+#pragma unroll
+                    for (int hf = 0; hf < PT / 2; ++hf) {
+                        const float pv[8] = {s[2 * hf][0], s[2 * hf][1], s[2 * hf][2], s[2 * hf][3], s[2 * hf + 1][0], s[2 * hf + 1][1], s[2 * hf + 1][2], s[2 * hf + 1][3]};
+                        bf16x8_t pb[NP];
+                        battn_planes<NP>(pv, pb);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d)
+#pragma unroll
+                            for (int q = NP - 1; q >= 0; --q)
+                                o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vf[hf][d]), pb[q], o[t][d], 0, 0, 0);
+                    }
+                    if (NT > 1) __builtin_amdgcn_sched_barrier(0);      // one tile after the other: their scores would not fit side by side
+                }
+            }
+        }
+
+        // the wavefronts' shares of each tile: thread (pair, dimensions) adds them up and writes them out, or leaves them for the merge
+        const bool whole = b0 == 0 && b1 == f.blocks;
+        float *slot = slots + (size_t)(2 * w + (b0 == 0)) * battn_few_slot<HD>(PAIRS);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            l[t] += lane_xor(l[t], 16);
+            l[t] += lane_xor(l[t], 32);
+            float *mine = mb + (wave * 16 + n16) * MROW;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int d = 0; d < DT; d += 4)
+                    *reinterpret_cast<f32x4_t *>(mine + DT * (4 * kg + q) + d) = f32x4_t{o[t][d][q], o[t][d + 1][q], o[t][d + 2][q], o[t][d + 3][q]};
+            if (kg == 0) { mine[HD] = off[t]; mine[HD + 1] = l[t]; }
+            __syncthreads();
+            constexpr int V = HD * PW / 16, TP = HD / V;      // values per thread, threads per pair
+            const int q16 = tid / TP, p = (q16 >> 4) * 16 * NT + t * 16 + (q16 & 15), d0 = (tid % TP) * V;
+            const float *share = mb + ((q16 >> 4) * 16 + (q16 & 15)) * MROW;         // of the first of the wavefronts that have this pair
+            float top = -INFINITY, sum = 0.f, v[V];
+#pragma unroll
+            for (int x = 0; x < 4; x += PW) top = fmaxf(top, share[x * 16 * MROW + HD]);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = 0.f;
+#pragma unroll
+            for (int x = 0; x < 4; x += PW) {
+                const float *m = share + x * 16 * MROW;
+                const float k = m[HD] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[HD] - top);
+                sum = fmaf(m[HD + 1], k, sum);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = fmaf(m[d0 + e], k, v[e]);
+            }
+            if (p < pairs) {
+                if (whole) {
+                    battn_few_out<V, HD, NP>(a, r0, kvh, pg * PAIRS + p, d0, v, sum);
+                } else {
+                    float *to = slot + p * MROW;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) __hip_atomic_store(to + d0 + e, v[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    if (d0 == 0) {
+                        __hip_atomic_store(to + HD, top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        __hip_atomic_store(to + HD + 1, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        if (!whole) {
+            const long long g0 = unit - b0;                   // the group's first unit
+            const int wa = run_of(g0), wb = run_of(g0 + f.blocks - 1);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's part of the partial result is in memory
+            __syncthreads();
+            if (tid == 0) ticket = __hip_atomic_fetch_add(counters + wa, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();
+            if (ticket == wb - wa) {                          // all the others are there
+                if (tid == 0) __hip_atomic_store(counters + wa, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                constexpr int V = HD / 16;
+                const int d0 = (tid & 15) * V;
+                for (int p = tid >> 4; p < pairs; p += 16) {
+                    float top = -INFINITY, sum = 0.f, v[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[e] = 0.f;
+                    for (int x = wa; x <= wb; ++x) {
+                        const float *m = slots + (size_t)(2 * x + (x == wa)) * battn_few_slot<HD>(PAIRS) + p * MROW;
+                        const float mx = __hip_atomic_load(m + HD, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), lx = __hip_atomic_load(m + HD + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        const float now = fmaxf(top, mx), k0 = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now), k1 = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - now);
+                        top = now;
+                        sum = sum * k0 + lx * k1;
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[e] = v[e] * k0 + __hip_atomic_load(m + d0 + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) * k1;
+                    }
+                    battn_few_out<V, HD, NP>(a, r0, kvh, pg * PAIRS + p, d0, v, sum);
+                }
+            }
+        }
+        unit += b1 - b0;
     }
 }
 

@@ -208,8 +208,13 @@ template <int N> __device__ __forceinline__ void store_values(float *p, const fl
     for (int i = 0; i < N; i += 4) *reinterpret_cast<float4 *>(p + i) = float4{v[i], v[i + 1], v[i + 2], v[i + 3]};
 }
 template <int N> __device__ __forceinline__ void store_values(bf16_t *p, const float *v) {
-    if constexpr (N == 8) *reinterpret_cast<uint4 *>(p) = uint4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-    else *reinterpret_cast<uint2 *>(p) = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    if constexpr (N >= 8) {
+#pragma unroll
+        for (int i = 0; i < N; i += 8)
+            *reinterpret_cast<uint4 *>(p + i) = uint4{pack_bf16(v[i], v[i + 1]), pack_bf16(v[i + 2], v[i + 3]), pack_bf16(v[i + 4], v[i + 5]), pack_bf16(v[i + 6], v[i + 7])};
+    } else {
+        *reinterpret_cast<uint2 *>(p) = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    }
 }
 
 template <int HD, typename T, typename KT>

@@ -81,23 +81,55 @@ static int32_t rows_check(const int32_t *row_start_dev, int32_t n_requests, cons
 }
 
 template <int HD, bool PAGED>
-static void launch_battn(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, hipStream_t s) {
-    if (dtype == KNNSSD_BF16) {
-        const int64_t tiles = ((int64_t)a.n_rows * a.group + BT_PAIRS - 1) / BT_PAIRS + a.n_requests;       // (at most; what is too much ends at once)
-        hipLaunchKernelGGL((battn_tile_kernel<HD, PAGED>), dim3((unsigned)(tiles * a.Hkv)), dim3(256), battn_tile_lds<HD>(), s, a);
+static void launch_tiles(const BattnArgs &a, hipStream_t s) {
+    const int64_t tiles = ((int64_t)a.n_rows * a.group + BT_PAIRS - 1) / BT_PAIRS + a.n_requests;       // (at most; what is too much ends at once)
+    hipLaunchKernelGGL((battn_tile_kernel<HD, PAGED>), dim3((unsigned)(tiles * a.Hkv)), dim3(256), battn_tile_lds<HD>(), s, a);
+}
+
+// most (row, head) pairs of one kv head for which a request goes through battn_few_kernel where battn_tile_kernel is there too
+static const int FEW_PAIRS = 64;
+
+template <int HD, int NT, int PW, int NP>
+static void launch_few(const BattnArgs &a, hipStream_t s) {
+    const int ch = battn_few_positions<HD>(NT);
+    const int64_t blocks = (((int64_t)a.width << a.shift) + ch - 1) / ch, groups = ((int64_t)a.n_rows * a.group + 16 * NT * PW - 1) / (16 * NT * PW) + a.n_requests;
+    const int64_t units = blocks < INT32_MAX ? blocks * groups * a.Hkv : INT64_MAX;      // at most
+    hipLaunchKernelGGL((battn_few_kernel<HD, NT, PW, NP>), dim3((unsigned)(units / 4 + 1 < BF_WGS ? units / 4 + 1 : BF_WGS)), dim3(256), (battn_few_lds<HD, NT, PW, NP>()), s, a);
+}
+
+// attention over a bf16 cache
+template <int HD>
+static void launch_paged_bf16(BattnArgs a, int32_t dtype, int32_t most_rows, hipStream_t s) {
+    const int64_t most = (int64_t)(most_rows > 0 && most_rows < a.n_rows ? most_rows : a.n_rows) * a.group;
+    a.few_rows = INT_MAX;
+    if (dtype == KNNSSD_FP32) {
+        if (most <= 16) launch_few<HD, 1, 1, 3>(a, s);
+        else launch_few<HD, 2, 1, 3>(a, s);
         return;
     }
+    if (most > FEW_PAIRS) a.few_rows = FEW_PAIRS / a.group;
+    if (a.few_rows > 0) {
+        if (most <= 16) launch_few<HD, 1, 1, 1>(a, s);
+        else if (most <= 32) launch_few<HD, 2, 1, 1>(a, s);
+        else launch_few<HD, 2, 2, 1>(a, s);
+    }
+    if (most > FEW_PAIRS) launch_tiles<HD, true>(a, s);
+}
+
+template <int HD, bool PAGED>
+static void launch_battn(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, int32_t most_rows, hipStream_t s) {
+    if (!PAGED && dtype == KNNSSD_BF16) return launch_tiles<HD, false>(a, s);
+    if (PAGED && kv_dtype == KNNSSD_BF16) return launch_paged_bf16<HD>(a, dtype, most_rows, s);
     const int64_t items = (int64_t)a.n_rows * a.H;
-    const dim3 grid((unsigned)((items + 3) / 4));
-    if (dtype == KNNSSD_BF16) hipLaunchKernelGGL((battn_row_kernel<HD, PAGED, bf16_t, bf16_t>), grid, dim3(256), 0, s, a);
-    else if (kv_dtype == KNNSSD_FP32) hipLaunchKernelGGL((battn_row_kernel<HD, PAGED, float, float>), grid, dim3(256), 0, s, a);
-    else if constexpr (PAGED) hipLaunchKernelGGL((battn_row_kernel<HD, PAGED, float, bf16_t>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((battn_row_kernel<HD, PAGED>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
 }
 
 extern "C" size_t knnssd_paged_attention_bytes(const knnssd_pages *p, int32_t n_heads, int32_t dtype) {
     if (pages_check(p) != KNNSSD_OK || !dtype_ok(dtype) || !types_go_together(dtype, p->kv_dtype)) return 0;
     if (n_heads < 1 || n_heads > 65535 || n_heads % p->n_kv_heads) return 0;
-    return 256;
+    if (p->kv_dtype == KNNSSD_FP32) return 256;
+    const size_t slot = p->head_dim == 128 ? battn_few_slot<128>(FEW_PAIRS) : battn_few_slot<64>(FEW_PAIRS);
+    return battn_few_counters() + 2 * BF_WGS * slot * sizeof(float);
 }
 
 extern "C" int32_t knnssd_paged_attention(const knnssd_pages *p, const int32_t *block_table_dev, int32_t table_width,
@@ -117,8 +149,9 @@ extern "C" int32_t knnssd_paged_attention(const knnssd_pages *p, const int32_t *
     a.n_requests = n_requests; a.n_rows = n_rows; a.width = table_width; a.shift = log2_of(p->page_size); a.n_pages = p->n_pages;
     a.H = n_heads; a.Hkv = p->n_kv_heads; a.group = n_heads / p->n_kv_heads;
     a.scale2 = scale * 1.4426950408889634f;
-    if (p->head_dim == 128) launch_battn<128, true>(a, dtype, p->kv_dtype, (hipStream_t)hip_stream);
-    else launch_battn<64, true>(a, dtype, p->kv_dtype, (hipStream_t)hip_stream);
+    a.ws = ws_dev;
+    if (p->head_dim == 128) launch_battn<128, true>(a, dtype, p->kv_dtype, most_rows, (hipStream_t)hip_stream);
+    else launch_battn<64, true>(a, dtype, p->kv_dtype, most_rows, (hipStream_t)hip_stream);
     HIP_TRY(hipGetLastError());
     return KNNSSD_OK;
 }
@@ -137,8 +170,8 @@ extern "C" int32_t knnssd_prompt_attention(const void *q_dev, int64_t q_stride, 
     a.row_start = row_start_dev; a.n_requests = n_requests; a.n_rows = n_rows;
     a.H = n_heads; a.Hkv = n_kv_heads; a.group = n_heads / n_kv_heads;
     a.scale2 = scale * 1.4426950408889634f;
-    if (head_dim == 128) launch_battn<128, false>(a, dtype, dtype, (hipStream_t)hip_stream);
-    else launch_battn<64, false>(a, dtype, dtype, (hipStream_t)hip_stream);
+    if (head_dim == 128) launch_battn<128, false>(a, dtype, dtype, 0, (hipStream_t)hip_stream);
+    else launch_battn<64, false>(a, dtype, dtype, 0, (hipStream_t)hip_stream);
     HIP_TRY(hipGetLastError());
     return KNNSSD_OK;
 }
