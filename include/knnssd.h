@@ -373,8 +373,8 @@ int32_t knnssd_paged_store(const knnssd_pages *pages, const void *qkv_dev, int32
  * bf16 for the product with the values. Positions from kv_len on are not looked at; keys and values that a row does not see but a
  * later one of its request does have to be finite. block_table_dev: [n_requests][table_width]. most_rows: an upper bound of a request's rows
  * if the caller has one, else 0; it only chooses the kernels. How the sums over a row are grouped follows the batch; the same call gives the
- * same bits. ws_dev: knnssd_paged_attention_bytes of the same pages, n_heads and dtype (0: not a supported shape), 256-byte aligned, ZEROED
- * ONCE before its first use; each call leaves it so that the next call, of whatever batch and shape that it is large enough for, can use it.
+ * same bits. ws_dev: knnssd_paged_attention_bytes of the same pages, n_heads and dtype (0: not a supported shape), 256-byte aligned, of any
+ * contents; nothing in it outlives a call.
  * KNNSSD_ESHAPE where n_heads is not a multiple of n_kv_heads, KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows < 1 or
  * n_rows * n_heads > KNNSSD_MAX_ROW_HEADS, table_width < 1 or a scale that is not finite. Lengths beyond 2^30 are taken as 2^30. */
 size_t knnssd_paged_attention_bytes(const knnssd_pages *pages, int32_t n_heads, int32_t dtype);

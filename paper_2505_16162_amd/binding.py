@@ -326,12 +326,12 @@ def knnssd_paged_store(pages: Pages, qkv: torch.Tensor, slots: torch.Tensor, pos
 
 
 def paged_attention_workspace(pages: Pages, n_heads: int, dtype: torch.dtype) -> torch.Tensor:
-    """A workspace for knnssd_paged_attention on these pages with n_heads query heads of `dtype` (zeroed once, here)."""
+    """A workspace for knnssd_paged_attention on these pages with n_heads query heads of `dtype`."""
     code = _TORCH_CODE.get(dtype)
     size = load_library().knnssd_paged_attention_bytes(pages.ref, int(n_heads), -1 if code is None else code)
     if size == 0:
         raise KnnSsdError(-2, "shape not supported")
-    return torch.zeros(size, dtype=torch.uint8, device=pages.device)
+    return torch.empty(size, dtype=torch.uint8, device=pages.device)
 
 
 def knnssd_paged_attention(pages: Pages, block_table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor, q: torch.Tensor, workspace: torch.Tensor,

@@ -1,5 +1,7 @@
 // Attention of a batch's rows over pages (PAGED) or over their own prompts' rows.
 #pragma once
+#include <type_traits>
+
 #include "kernels_pages.h"
 
 namespace ks {
@@ -328,25 +330,27 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
 
 // ------------------------------------------------------------------------------------------
 // Few rows over a bf16 cache: what bounds them is the cache, read once. A request's (row, head) pairs of one kv head, 16 NT at a time, against
-// all of its positions are a group; a group's blocks of 64 (32 where more pairs share them) positions are units, and the units of the whole batch, group behind
+// all of its positions are a group; a group's blocks of 32 (heads of 64: 64) positions are units, and the units of the whole batch, group behind
 // group, are dealt to the workgroups in equal runs (worked out by each for itself from the lengths). The four wavefronts of a workgroup take the
 // blocks of a run in turn, keys and values straight from the cache to registers as operands, and are merged in LDS where a group ends. A
-// group that lies in several runs leaves a partial result per run in the workspace, and the workgroup that counts itself in last merges them,
-// in the order of the runs. Nobody waits for anybody; the counter goes back to zero.
+// group that lies in several runs leaves a partial result per run in the workspace; battn_merge_kernel joins them, in the order of the runs.
 // As in the tile kernel everything is transposed, here in 16 x 16 tiles. Values are regrouped by byte permutes: a lane takes HD/16 neighbouring
 // dimensions of its eight positions, so that matrix instruction t yields dimensions {HD/16 n + t}.
 // NP = 3: fp32 queries, which stay exact as three bf16 planes, as do the weights.
 // ------------------------------------------------------------------------------------------
-constexpr int BF_WGS = 512;                                   // two workgroups per compute unit: 256 KB of the cache in flight on each
+constexpr int BF_WGS = 512;                                   // two workgroups per compute unit: 128 KB of the cache in flight on each
 constexpr int BF_PAD = 4;                                     // floats behind a pair's HD values: its exponent, its sum
 
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-// positions of a unit: what a wavefront holds in registers beside its accumulators
-template <int HD> __host__ __device__ constexpr int battn_few_positions(int nt) { return HD == 128 && nt > 1 ? 32 : 64; }
+// positions of a unit: 8 KB of keys, 8 KB of values, which a wavefront holds in registers
+template <int HD> __host__ __device__ constexpr int battn_few_positions() { return 32 * 128 / HD; }
 template <int HD> __host__ __device__ constexpr size_t battn_few_slot(int pairs) { return (size_t)pairs * (HD + BF_PAD); }      // floats of a partial result
-__host__ __device__ constexpr size_t battn_few_counters() { return BF_WGS * sizeof(int); }
+// a group that begins in a run and does not end there: the runs that hold it, its first row's request, kv head, first pair and pairs
+struct FewMerge { int runs, r0, kvh, pair, pairs; };
+__host__ __device__ constexpr size_t battn_few_merges() { return BF_WGS * 32; }
+static_assert(sizeof(FewMerge) <= 32, "");
 
 // eight fp32 values as NP bf16 operands: rounded to nearest (1), or cut three times into exact parts (3)
 template <int NP>
@@ -369,6 +373,11 @@ __device__ __forceinline__ void battn_planes(const float *v, bf16x8_t *out) {
             out[p] = __builtin_bit_cast(bf16x8_t, w);
         }
     }
+}
+
+// lane i's value, known to be the same everywhere (scalar registers, scalar loads)
+__device__ __forceinline__ long long battn_lane(long long v, int i) {
+    return (long long)(unsigned int)__builtin_amdgcn_readlane((int)v, i) | (long long)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32;
 }
 
 // units of request r: rows (0: not this kernel's), blocks of a group, groups of pairs per kv head
@@ -397,23 +406,30 @@ __device__ __forceinline__ void battn_few_out(const BattnArgs &a, int r0, int kv
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] *= inv;
     const long long at = (long long)(r0 + pair / a.group) * a.out_stride + (kvh * a.group + pair % a.group) * HD + d;
-    if constexpr (NP == 1) store_values<V>((bf16_t *)a.out + at, v);
-    else store_values<V>((float *)a.out + at, v);
+    if constexpr (V >= 4) {
+        if constexpr (NP == 1) store_values<V>((bf16_t *)a.out + at, v);
+        else store_values<V>((float *)a.out + at, v);
+    } else if constexpr (NP == 1) {
+        if constexpr (V == 2) *reinterpret_cast<unsigned int *>((bf16_t *)a.out + at) = pack_bf16(v[0], v[1]);
+        else ((bf16_t *)a.out)[at] = (bf16_t)pack_bf16(v[0], 0.f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) ((float *)a.out)[at + e] = v[e];
+    }
 }
 
 template <int HD, int NT, int PW, int NP>
 __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
-    constexpr int QS = HD / 32, DT = HD / 16, QROW = HD + 8, MROW = HD + BF_PAD, PAIRS = 16 * NT * PW, CH = battn_few_positions<HD>(NT), PT = CH / 16;
+    constexpr int QS = HD / 32, DT = HD / 16, QROW = HD + 8, MROW = HD + BF_PAD, PAIRS = 16 * NT * PW, CH = battn_few_positions<HD>(), PT = CH / 16;
     typedef unsigned int vword __attribute__((ext_vector_type(DT / 2)));
     extern __shared__ __align__(16) char lds[];
-    __shared__ int ticket;
     bf16_t *ql = (bf16_t *)lds;
     float *mb = (float *)(lds + NP * PAIRS * QROW * 2);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kg = lane >> 4, n16 = lane & 15;
     const int wp = wave % PW, wb = wave / PW, wave_pair = wp * 16 * NT;      // the wavefront's pairs, its blocks: wb, wb + 4/PW, ...
-    float *slots = (float *)((char *)a.ws + battn_few_counters());
-    int *counters = (int *)a.ws;
+    float *slots = (float *)((char *)a.ws + battn_few_merges());
+    FewMerge *merges = (FewMerge *)a.ws;
 
     // all units, and the first of this workgroup's run: how many requests lie before it, their units
     long long total = 0;
@@ -425,10 +441,11 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
             mine = (long long)f.blocks * f.pair_groups * a.Hkv;
         }
         for (int off = 32; off; off >>= 1) mine += __shfl_xor(mine, off);
-        total += mine;
+        total += battn_lane(mine, 0);
     }
     const int runs = (int)min((long long)gridDim.x, (total + 3) / 4);           // four units at least: a block for every wavefront
     const int w = blockIdx.x;
+    if (tid == 0) merges[w] = FewMerge{0, 0, 0, 0, 0};
     if (w >= runs) return;
     auto run_start = [&](int i) { return (long long)i * total / runs; };
     auto run_of = [&](long long unit) { return (int)(((unit + 1) * runs - 1) / total); };
@@ -452,12 +469,11 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
             if (past) {
                 const int src = __builtin_ctzll(past);
                 r = r0 + src;
-                if (src > 0) before += __shfl(upto, src - 1);
+                if (src > 0) before += battn_lane(upto, src - 1);
                 break;
             }
-            before += __shfl(upto, 63);
+            before += battn_lane(upto, 63);
         }
-        r = __builtin_amdgcn_readfirstlane(r);
         f = battn_few_shape(a, r, PAIRS, CH);
     }
     const float c2 = fabsf(a.scale2);
@@ -511,105 +527,147 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
         const int first_limit = base + pg * PAIRS / a.group;
         const const_ints table = (const_ints)(uintptr_t)(a.table + (size_t)r * a.width);
         const bf16_t *kb = (const bf16_t *)a.k + kvh * a.head_stride, *vb = (const bf16_t *)a.v + kvh * a.head_stride;
-        if (len > 0) {
-            for (int b = b0 + wb; b < b1 && wave_pair < pairs; b += 4 / PW) {
-                const int pos0 = b * CH;
-                u32x4_t kf[PT][QS];                            // position 16 pt + n16, dimensions 32 ks + 8 kg ...
-                vword vr[PT][4];                               // position 16 pt + 4 kg + i, dimensions DT n16 ...
+        // A block's keys and values are requested while the block before it is worked on, its pages one block earlier still.
+        u32x4_t kf[PT][QS];                                   // position 16 pt + n16, dimensions 32 ks + 8 kg ...
+        vword vr[PT][4];                                      // position 16 pt + 4 kg + i, dimensions DT n16 ...
+        int page[PT][2];
+        // first position of the block's e-th eight of tile pt (a page holds at least eight); positions past the last one repeat it
+        auto eight = [&](int b, int pt, int e) __attribute__((always_inline)) { return min(b * CH + pt * 16 + e * 8, last & -8); };
+        auto look_up = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
-                for (int pt = 0; pt < PT; ++pt) {
-                    // the tile's positions eight by eight: a page holds at least so many. Positions past the last one repeat it.
-                    long long at[2];
-                    int in8[2], rest[2];
+            for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int p = min(pos0 + pt * 16 + e * 8, last & -8), id = table[p >> a.shift];
-                        at[e] = ((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.page_stride + (p & ((1 << a.shift) - 1)) * a.pos_stride;
-                        rest[e] = last - p;
+                for (int e = 0; e < 2; ++e) page[pt][e] = table[eight(b, pt, e) >> a.shift];
+        };
+        auto offset = [&](int b, int pt, int e) __attribute__((always_inline)) {
+            const int id = __builtin_amdgcn_readfirstlane(page[pt][e]);      // (or a lane's choice between two becomes an index into memory)
+            return ((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.page_stride + (eight(b, pt, e) & ((1 << a.shift) - 1)) * a.pos_stride;
+        };
+        auto load_keys = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+            for (int pt = 0; pt < PT; ++pt) {
+                const long long lo = offset(b, pt, 0), hi = offset(b, pt, 1);
+                const int in8 = min(n16 & 7, last - (n16 & 8 ? eight(b, pt, 1) : eight(b, pt, 0)));
+                const bf16_t *kp = kb + (n16 & 8 ? hi : lo) + in8 * a.pos_stride + kg * 8;
+#pragma unroll
+                for (int ks = 0; ks < QS; ++ks) kf[pt][ks] = *reinterpret_cast<const u32x4_t *>(kp + ks * 32);
+            }
+        };
+        auto load_values = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+            for (int pt = 0; pt < PT; ++pt) {
+                const long long lo = offset(b, pt, 0), hi = offset(b, pt, 1);
+                const int rest = last - (kg & 2 ? eight(b, pt, 1) : eight(b, pt, 0));
+                const bf16_t *vp = vb + (kg & 2 ? hi : lo) + n16 * DT;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) vr[pt][i] = *reinterpret_cast<const vword *>(vp + min((kg & 1) * 4 + i, rest) * a.pos_stride);
+            }
+        };
+        constexpr int STEP = 4 / PW;
+        const bool any = len > 0 && wave_pair < pairs && b0 + wb < b1;
+        if (any) {
+            look_up(b0 + wb);
+            load_keys(b0 + wb);
+            load_values(b0 + wb);
+            look_up(b0 + wb + STEP);
+        }
+        // (two builds, with a next block and without: what is in flight where a value is waited for has to be known)
+        auto work = [&](int b, auto more_) __attribute__((always_inline)) {
+            constexpr bool more = decltype(more_)::value;
+            const int pos0 = b * CH;
+            const bool diagonal = pos0 + CH - 1 > first_limit;
+            f32x4_t s[NT][PT];
+            const bf16_t *qb = ql + (wave_pair + n16) * QROW + kg * 8;
+            if (NT * NP > 1) asm volatile("" : "+v"(qb));     // (they are read again for every block: there is no room to keep them all)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int pt = 0; pt < PT; ++pt) s[t][pt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                // the lowest plane first
+#pragma unroll
+                for (int q = NP - 1; q >= 0; --q)
+#pragma unroll
+                    for (int ks = 0; ks < QS; ++ks) {
+                        const bf16x8_t qf = *reinterpret_cast<const bf16x8_t *>(qb + (q * PAIRS + t * 16) * QROW + ks * 32);
+#pragma unroll
+                        for (int pt = 0; pt < PT; ++pt) s[t][pt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[pt][ks]), qf, s[t][pt], 0, 0, 0);
                     }
-                    in8[0] = min(n16 & 7, n16 & 8 ? rest[1] : rest[0]);
-                    const bf16_t *kp = kb + (n16 & 8 ? at[1] : at[0]) + in8[0] * a.pos_stride + kg * 8;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (more) load_keys(b + STEP);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int ks = 0; ks < QS; ++ks) kf[pt][ks] = *reinterpret_cast<const u32x4_t *>(kp + ks * 32);
-                    const bf16_t *vp = vb + (kg & 2 ? at[1] : at[0]) + n16 * DT;
-                    const int vrest = kg & 2 ? rest[1] : rest[0];
+            for (int t = 0; t < NT; ++t) {
+                if (diagonal) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) vr[pt][i] = *reinterpret_cast<const vword *>(vp + min((kg & 1) * 4 + i, vrest) * a.pos_stride);
+                    for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (pos0 + pt * 16 + 4 * kg + i > limit[t]) s[t][pt][i] = -INFINITY;
                 }
-                __builtin_amdgcn_sched_barrier(0);            // every load is on its way before the first is waited for
-                const bool diagonal = pos0 + CH - 1 > first_limit;
-                u32x4_t vf[PT / 2][DT];
+                float cm = s[t][0][0];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    if (wave_pair + t * 16 >= pairs) break;
-                    f32x4_t s[PT];
+                for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
-                    for (int pt = 0; pt < PT; ++pt) s[pt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-                    // the lowest plane first
+                    for (int i = 0; i < 4; ++i) cm = fmaxf(cm, s[t][pt][i]);
+                cm = fmaxf(cm, lane_xor(cm, 16));
+                cm = fmaxf(cm, lane_xor(cm, 32));
+                // (-inf times a scale of 0 would be NaN)
+                const float off_new = cm == -INFINITY ? off[t] : fmaxf(off[t], battn_rounded_product(cm, c2)), ref = off_new == -INFINITY ? 0.f : off_new;
+                const float fac = __builtin_amdgcn_exp2f(off[t] - ref);
+                off[t] = off_new;
+                float ps = 0.f;
 #pragma unroll
-                    for (int q = NP - 1; q >= 0; --q)
+                for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
-                        for (int ks = 0; ks < QS; ++ks) {
-                            const bf16x8_t qf = *reinterpret_cast<const bf16x8_t *>(ql + (q * PAIRS + wave_pair + t * 16 + n16) * QROW + ks * 32 + kg * 8);
-#pragma unroll
-                            for (int pt = 0; pt < PT; ++pt) s[pt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[pt][ks]), qf, s[pt], 0, 0, 0);
-                        }
-                    if (diagonal) {
-#pragma unroll
-                        for (int pt = 0; pt < PT; ++pt)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (pos0 + pt * 16 + 4 * kg + i > limit[t]) s[pt][i] = -INFINITY;
+                    for (int i = 0; i < 4; ++i) {
+                        s[t][pt][i] = __builtin_amdgcn_exp2f(fmaf(s[t][pt][i], c2, -ref));
+                        if (diagonal && pos0 + pt * 16 + 4 * kg + i > limit[t]) s[t][pt][i] = 0.f;
+                        ps += s[t][pt][i];
                     }
-                    float cm = s[0][0];
+                l[t] = l[t] * fac + ps;
+                if (__any(fac != 1.0f)) {
 #pragma unroll
-                    for (int pt = 0; pt < PT; ++pt)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) cm = fmaxf(cm, s[pt][i]);
-                    cm = fmaxf(cm, lane_xor(cm, 16));
-                    cm = fmaxf(cm, lane_xor(cm, 32));
-                    // (-inf times a scale of 0 would be NaN)
-                    const float off_new = cm == -INFINITY ? off[t] : fmaxf(off[t], battn_rounded_product(cm, c2)), ref = off_new == -INFINITY ? 0.f : off_new;
-                    const float fac = __builtin_amdgcn_exp2f(off[t] - ref);
-                    off[t] = off_new;
-                    float ps = 0.f;
-#pragma unroll
-                    for (int pt = 0; pt < PT; ++pt)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            s[pt][i] = __builtin_amdgcn_exp2f(fmaf(s[pt][i], c2, -ref));
-                            if (diagonal && pos0 + pt * 16 + 4 * kg + i > limit[t]) s[pt][i] = 0.f;
-                            ps += s[pt][i];
-                        }
-                    l[t] = l[t] * fac + ps;
-                    if (__any(fac != 1.0f)) {
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) o[t][d] *= fac;
-                    }
-                    if (t == 0) {                             // the values' operands, once for all tiles: positions 2j, 2j+1 of the lane's eight
-#pragma unroll
-                        for (int hf = 0; hf < PT / 2; ++hf)
-#pragma unroll
-                            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                                for (int j = 0; j < 4; ++j)
-                                    vf[hf][d][j] = __builtin_amdgcn_perm(vr[2 * hf + (j >> 1)][2 * (j & 1) + 1][d >> 1], vr[2 * hf + (j >> 1)][2 * (j & 1)][d >> 1],
-                                                                         (d & 1) ? 0x07060302u : 0x05040100u);
-                    }
-#pragma unroll
-                    for (int hf = 0; hf < PT / 2; ++hf) {
-                        const float pv[8] = {s[2 * hf][0], s[2 * hf][1], s[2 * hf][2], s[2 * hf][3], s[2 * hf + 1][0], s[2 * hf + 1][1], s[2 * hf + 1][2], s[2 * hf + 1][3]};
-                        bf16x8_t pb[NP];
-                        battn_planes<NP>(pv, pb);
-#pragma unroll
-                        for (int d = 0; d < DT; ++d)
-#pragma unroll
-                            for (int q = NP - 1; q >= 0; --q)
-                                o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vf[hf][d]), pb[q], o[t][d], 0, 0, 0);
-                    }
-                    if (NT > 1) __builtin_amdgcn_sched_barrier(0);      // one tile after the other: their scores would not fit side by side
+                    for (int d = 0; d < DT; ++d) o[t][d] *= fac;
                 }
             }
+            u32x4_t vf[PT / 2][DT];                           // the values' operands: positions 2j, 2j+1 of the lane's eight
+#pragma unroll
+            for (int hf = 0; hf < PT / 2; ++hf)
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        vf[hf][d][j] = __builtin_amdgcn_perm(vr[2 * hf + (j >> 1)][2 * (j & 1) + 1][d >> 1], vr[2 * hf + (j >> 1)][2 * (j & 1)][d >> 1],
+                                                             (d & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int hf = 0; hf < PT / 2; ++hf)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) asm volatile("" : "+v"(vf[hf][d]));       // all of it here: the next values go to the same registers
+            if constexpr (more) {
+                load_values(b + STEP);
+                look_up(b + 2 * STEP);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int hf = 0; hf < PT / 2; ++hf) {
+                    const f32x4_t x = s[t][2 * hf], y = s[t][2 * hf + 1];
+                    const float pv[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+                    bf16x8_t pb[NP];
+                    battn_planes<NP>(pv, pb);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int q = NP - 1; q >= 0; --q)
+                            o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vf[hf][d]), pb[q], o[t][d], 0, 0, 0);
+                }
+        };
+        if (any) {
+            int b = b0 + wb;
+            for (; b + STEP < b1; b += STEP) work(b, std::true_type{});
+            work(b, std::false_type{});
         }
 
         // the wavefronts' shares of each tile: thread (pair, dimensions) adds them up and writes them out, or leaves them for the merge
@@ -648,45 +706,79 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
                     battn_few_out<V, HD, NP>(a, r0, kvh, pg * PAIRS + p, d0, v, sum);
                 } else {
                     float *to = slot + p * MROW;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) __hip_atomic_store(to + d0 + e, v[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    if (d0 == 0) {
-                        __hip_atomic_store(to + HD, top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        __hip_atomic_store(to + HD + 1, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    }
+                    store_values<V>(to + d0, v);
+                    if (d0 == 0) { to[HD] = top; to[HD + 1] = sum; }
                 }
             }
             __syncthreads();
         }
-        if (!whole) {
-            const long long g0 = unit - b0;                   // the group's first unit
-            const int wa = run_of(g0), wb = run_of(g0 + f.blocks - 1);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's part of the partial result is in memory
-            __syncthreads();
-            if (tid == 0) ticket = __hip_atomic_fetch_add(counters + wa, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __syncthreads();
-            if (ticket == wb - wa) {                          // all the others are there
-                if (tid == 0) __hip_atomic_store(counters + wa, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                constexpr int V = HD / 16;
-                const int d0 = (tid & 15) * V;
-                for (int p = tid >> 4; p < pairs; p += 16) {
-                    float top = -INFINITY, sum = 0.f, v[V];
-#pragma unroll
-                    for (int e = 0; e < V; ++e) v[e] = 0.f;
-                    for (int x = wa; x <= wb; ++x) {
-                        const float *m = slots + (size_t)(2 * x + (x == wa)) * battn_few_slot<HD>(PAIRS) + p * MROW;
-                        const float mx = __hip_atomic_load(m + HD, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), lx = __hip_atomic_load(m + HD + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        const float now = fmaxf(top, mx), k0 = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now), k1 = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - now);
-                        top = now;
-                        sum = sum * k0 + lx * k1;
-#pragma unroll
-                        for (int e = 0; e < V; ++e) v[e] = v[e] * k0 + __hip_atomic_load(m + d0 + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) * k1;
-                    }
-                    battn_few_out<V, HD, NP>(a, r0, kvh, pg * PAIRS + p, d0, v, sum);
-                }
-            }
+        if (!whole && b0 == 0 && tid == 0) {
+            const long long g0 = unit;                        // the group's first unit: it goes on in the runs behind this one
+            merges[w] = FewMerge{run_of(g0 + f.blocks - 1) - w + 1, r0, kvh, pg * PAIRS, pairs};
         }
         unit += b1 - b0;
+    }
+}
+
+// Joins the partial results of a group: four wavefronts a pair, a quarter of the runs each (every fourth), four requested at a time. In a launch of its own: the last
+// workgroup of a group doing it inside the first launch had to fetch up to 32 runs' results of all pairs by itself, one memory
+// latency after the other (two requests at 100 000 positions: 286 us).
+constexpr int BM_NT = 1024, BM_PAIRS = 4;
+template <int HD, int NP>
+__global__ __launch_bounds__(BM_NT) void battn_merge_kernel(BattnArgs a, int slot_pairs) {
+    constexpr int V = HD / 64, MROW = HD + BF_PAD, U = 4;
+    __shared__ float part[BM_NT / 64][HD + 2];
+    const FewMerge m = ((const FewMerge *)a.ws)[blockIdx.x];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = wave & 3;
+    if (m.runs == 0) return;                                  // the whole workgroup
+    const size_t slot = battn_few_slot<HD>(slot_pairs);
+    for (int p0 = blockIdx.y * BM_PAIRS; p0 < m.pairs; p0 += gridDim.y * BM_PAIRS) {
+        const int p = p0 + (wave >> 2);
+        // run x's partial result is its second one (a group that begins there) for the first run, its first one for the others
+        const float *first = (const float *)((const char *)a.ws + battn_few_merges()) + 2 * blockIdx.x * slot + min(p, m.pairs - 1) * MROW;
+        float top = -INFINITY, sum = 0.f, v[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = 0.f;
+        for (int x = sub; x < m.runs; x += 4 * U) {
+            float at[U], l[U], w[U][V];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int y = min(x + 4 * u, m.runs - 1);
+                const float *from = first + (2 * y + (y == 0)) * slot;
+                at[u] = from[HD];
+                l[u] = from[HD + 1];
+#pragma unroll
+                for (int e = 0; e < V; ++e) w[u][e] = from[lane * V + e];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (x + 4 * u >= m.runs || at[u] == -INFINITY) continue;
+                const float now = fmaxf(top, at[u]), k0 = __builtin_amdgcn_exp2f(top - now), k1 = __builtin_amdgcn_exp2f(at[u] - now);
+                top = now;
+                sum = sum * k0 + l[u] * k1;
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = v[e] * k0 + w[u][e] * k1;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) part[wave][lane * V + e] = v[e];
+        if (lane == 0) { part[wave][HD] = top; part[wave][HD + 1] = sum; }
+        __syncthreads();
+        if (sub == 0 && p < m.pairs) {
+            top = fmaxf(fmaxf(part[wave][HD], part[wave + 1][HD]), fmaxf(part[wave + 2][HD], part[wave + 3][HD]));
+            sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = 0.f;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const float k = part[wave + x][HD] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part[wave + x][HD] - top);
+                sum = fmaf(part[wave + x][HD + 1], k, sum);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = fmaf(part[wave + x][lane * V + e], k, v[e]);
+            }
+            battn_few_out<V, HD, NP>(a, m.r0, m.kvh, m.pair + p, lane * V, v, sum);
+        }
+        __syncthreads();
     }
 }
 

@@ -90,11 +90,14 @@ static void launch_tiles(const BattnArgs &a, hipStream_t s) {
 static const int FEW_PAIRS = 64;
 
 template <int HD, int NT, int PW, int NP>
-static void launch_few(const BattnArgs &a, hipStream_t s) {
-    const int ch = battn_few_positions<HD>(NT);
+static void launch_few(const BattnArgs &a, int64_t most, hipStream_t s) {
+    const int ch = battn_few_positions<HD>();
     const int64_t blocks = (((int64_t)a.width << a.shift) + ch - 1) / ch, groups = ((int64_t)a.n_rows * a.group + 16 * NT * PW - 1) / (16 * NT * PW) + a.n_requests;
     const int64_t units = blocks < INT32_MAX ? blocks * groups * a.Hkv : INT64_MAX;      // at most
-    hipLaunchKernelGGL((battn_few_kernel<HD, NT, PW, NP>), dim3((unsigned)(units / 4 + 1 < BF_WGS ? units / 4 + 1 : BF_WGS)), dim3(256), (battn_few_lds<HD, NT, PW, NP>()), s, a);
+    const unsigned runs = (unsigned)(units / 4 + 1 < BF_WGS ? units / 4 + 1 : BF_WGS);
+    hipLaunchKernelGGL((battn_few_kernel<HD, NT, PW, NP>), dim3(runs), dim3(256), (battn_few_lds<HD, NT, PW, NP>()), s, a);
+    const int pairs = (int)(most < 16 * NT * PW ? most : 16 * NT * PW);
+    hipLaunchKernelGGL((battn_merge_kernel<HD, NP>), dim3(runs, (pairs + BM_PAIRS - 1) / BM_PAIRS), dim3(BM_NT), 0, s, a, 16 * NT * PW);
 }
 
 // attention over a bf16 cache
@@ -103,15 +106,15 @@ static void launch_paged_bf16(BattnArgs a, int32_t dtype, int32_t most_rows, hip
     const int64_t most = (int64_t)(most_rows > 0 && most_rows < a.n_rows ? most_rows : a.n_rows) * a.group;
     a.few_rows = INT_MAX;
     if (dtype == KNNSSD_FP32) {
-        if (most <= 16) launch_few<HD, 1, 1, 3>(a, s);
-        else launch_few<HD, 2, 1, 3>(a, s);
+        if (most <= 16) launch_few<HD, 1, 1, 3>(a, most, s);
+        else launch_few<HD, 2, 1, 3>(a, most, s);
         return;
     }
     if (most > FEW_PAIRS) a.few_rows = FEW_PAIRS / a.group;
     if (a.few_rows > 0) {
-        if (most <= 16) launch_few<HD, 1, 1, 1>(a, s);
-        else if (most <= 32) launch_few<HD, 2, 1, 1>(a, s);
-        else launch_few<HD, 2, 2, 1>(a, s);
+        if (most <= 16) launch_few<HD, 1, 1, 1>(a, most, s);
+        else if (most <= 32) launch_few<HD, 2, 1, 1>(a, most, s);
+        else launch_few<HD, 2, 2, 1>(a, most, s);
     }
     if (most > FEW_PAIRS) launch_tiles<HD, true>(a, s);
 }
@@ -129,7 +132,7 @@ extern "C" size_t knnssd_paged_attention_bytes(const knnssd_pages *p, int32_t n_
     if (n_heads < 1 || n_heads > 65535 || n_heads % p->n_kv_heads) return 0;
     if (p->kv_dtype == KNNSSD_FP32) return 256;
     const size_t slot = p->head_dim == 128 ? battn_few_slot<128>(FEW_PAIRS) : battn_few_slot<64>(FEW_PAIRS);
-    return battn_few_counters() + 2 * BF_WGS * slot * sizeof(float);
+    return battn_few_merges() + 2 * BF_WGS * slot * sizeof(float);
 }
 
 extern "C" int32_t knnssd_paged_attention(const knnssd_pages *p, const int32_t *block_table_dev, int32_t table_width,
