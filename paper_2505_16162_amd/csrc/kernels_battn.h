@@ -380,6 +380,20 @@ __device__ __forceinline__ long long battn_lane(long long v, int i) {
     return (long long)(unsigned int)__builtin_amdgcn_readlane((int)v, i) | (long long)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32;
 }
 
+// x / d for 0 <= x < 2^53 and d > 0: many times shorter than a division of 64-bit integers
+__device__ __forceinline__ long long battn_divide(long long x, long long d) {
+    long long q = (long long)((double)x / (double)d);
+    if (q * d > x) --q;
+    if ((q + 1) * d <= x) ++q;
+    return q;
+}
+
+// run that has a unit, where the first rem runs have q + 1 units and the others q
+__device__ __forceinline__ int battn_run_of(long long unit, long long q, long long rem) {
+    const long long longer = rem * (q + 1);
+    return (int)(unit < longer ? battn_divide(unit, q + 1) : rem + battn_divide(unit - longer, q));
+}
+
 // units of request r: rows (0: not this kernel's), blocks of a group, groups of pairs per kv head
 struct FewShape { int n, blocks, pair_groups; };
 __device__ __forceinline__ FewShape battn_few_shape(const BattnArgs &a, int r, int group_pairs, int positions) {
@@ -406,18 +420,11 @@ __device__ __forceinline__ void battn_few_out(const BattnArgs &a, int r0, int kv
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] *= inv;
     const long long at = (long long)(r0 + pair / a.group) * a.out_stride + (kvh * a.group + pair % a.group) * HD + d;
-    if constexpr (V >= 4) {
-        if constexpr (NP == 1) store_values<V>((bf16_t *)a.out + at, v);
-        else store_values<V>((float *)a.out + at, v);
-    } else if constexpr (NP == 1) {
-        if constexpr (V == 2) *reinterpret_cast<unsigned int *>((bf16_t *)a.out + at) = pack_bf16(v[0], v[1]);
-        else ((bf16_t *)a.out)[at] = (bf16_t)pack_bf16(v[0], 0.f);
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) ((float *)a.out)[at + e] = v[e];
-    }
+    if constexpr (NP == 1) store_values<V>((bf16_t *)a.out + at, v);
+    else store_values<V>((float *)a.out + at, v);
 }
 
+// PW: most wavefronts that share a block, where the pairs are more than one holds
 template <int HD, int NT, int PW, int NP>
 __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
     constexpr int QS = HD / 32, DT = HD / 16, QROW = HD + 8, MROW = HD + BF_PAD, PAIRS = 16 * NT * PW, CH = battn_few_positions<HD>(), PT = CH / 16;
@@ -427,35 +434,18 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
     float *mb = (float *)(lds + NP * PAIRS * QROW * 2);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kg = lane >> 4, n16 = lane & 15;
-    const int wp = wave % PW, wb = wave / PW, wave_pair = wp * 16 * NT;      // the wavefront's pairs, its blocks: wb, wb + 4/PW, ...
     float *slots = (float *)((char *)a.ws + battn_few_merges());
     FewMerge *merges = (FewMerge *)a.ws;
 
-    // all units, and the first of this workgroup's run: how many requests lie before it, their units
-    long long total = 0;
-    for (int r0 = 0; r0 < a.n_requests; r0 += 64) {
-        const int r = r0 + lane;
-        long long mine = 0;
-        if (r < a.n_requests) {
-            const FewShape f = battn_few_shape(a, r, PAIRS, CH);
-            mine = (long long)f.blocks * f.pair_groups * a.Hkv;
-        }
-        for (int off = 32; off; off >>= 1) mine += __shfl_xor(mine, off);
-        total += battn_lane(mine, 0);
-    }
-    const int runs = (int)min((long long)gridDim.x, (total + 3) / 4);           // four units at least: a block for every wavefront
+    // All units, the first of this workgroup's run, and the request that has it: how many units lie before that one's. Up to 64 requests are looked at once.
+    long long total = 0, before = 0, unit = 0, unit_end = 0, q = 0, rem = 0;
+    int r = 0, runs = 0;
     const int w = blockIdx.x;
     if (tid == 0) merges[w] = FewMerge{0, 0, 0, 0, 0};
-    if (w >= runs) return;
-    auto run_start = [&](int i) { return (long long)i * total / runs; };
-    auto run_of = [&](long long unit) { return (int)(((unit + 1) * runs - 1) / total); };
-    long long unit = run_start(w);
-    const long long unit_end = run_start(w + 1);
-    long long before = 0;                                     // units before request r
-    int r = 0;
-    FewShape f{0, 1, 0};
-    {
-        for (int r0 = 0; r0 < a.n_requests; r0 += 64) {
+    auto run_start = [&](int i) { return i * q + min((long long)i, rem); };      // rem runs of q + 1 units, the others of q
+    for (int pass = 0; pass < 2; ++pass) {
+        bool found = false;
+        for (int r0 = 0; r0 < a.n_requests && !found; r0 += 64) {
             long long upto = 0;
             if (r0 + lane < a.n_requests) {
                 const FewShape g = battn_few_shape(a, r0 + lane, PAIRS, CH);
@@ -465,50 +455,134 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
                 const long long u = __shfl_up(upto, off);
                 if (lane >= off) upto += u;
             }
-            const unsigned long long past = __ballot(unit < before + upto);
-            if (past) {
-                const int src = __builtin_ctzll(past);
-                r = r0 + src;
-                if (src > 0) before += battn_lane(upto, src - 1);
-                break;
+            if (pass == 0) total += battn_lane(upto, 63);
+            if (pass == 0 && r0 + 64 >= a.n_requests) {       // the total is known
+                runs = (int)min((long long)gridDim.x, (total + 3) / 4);         // four units at least: a block for every wavefront
+                if (w >= runs) return;
+                q = battn_divide(total, runs);
+                rem = total - q * runs;
+                unit = run_start(w);
+                unit_end = run_start(w + 1);
             }
-            before += battn_lane(upto, 63);
+            if (pass == 1 || a.n_requests <= 64) {
+                const unsigned long long past = __ballot(unit < before + upto);
+                found = past != 0;
+                if (found) {
+                    const int src = __builtin_ctzll(past);
+                    r = r0 + src;
+                    if (src > 0) before += battn_lane(upto, src - 1);
+                } else {
+                    before += battn_lane(upto, 63);
+                }
+            }
         }
-        f = battn_few_shape(a, r, PAIRS, CH);
+        if (found) break;
     }
     const float c2 = fabsf(a.scale2);
     const unsigned int flip = a.scale2 < 0.f ? 0x80000000u : 0u;
 
-    while (unit < unit_end) {
-        while (unit - before >= (long long)f.blocks * f.pair_groups * a.Hkv) {   // on to the next request with units
+    // Where the run is: a group, its blocks [b0, b1) of the run. What follows sets these for the blocks from `unit` on, and requests the group's
+    // queries and the wavefront's first block.
+    FewShape f = battn_few_shape(a, r, PAIRS, CH);
+    int kvh, pg, b0, b1, r0, len, last, pairs, wp, wb, step, wave_pair;
+    bool any;
+    const_ints table;
+    const bf16_t *kb, *vb;
+    u32x4_t kf[PT][QS];                                       // position 16 pt + n16, dimensions 32 ks + 8 kg ...
+    vword vr[PT][4];                                          // position 16 pt + 4 kg + i, dimensions DT n16 ...
+    int page[PT][2];
+    constexpr int NQ = (PAIRS * (HD / 8) + 255) / 256;        // 8 values of a query each: a thread's
+    u32x4_t qv[NQ][NP == 1 ? 1 : 2];
+    // first position of the block's e-th eight of tile pt (a page holds at least eight); positions past the last one repeat it
+    auto eight = [&](int b, int pt, int e) __attribute__((always_inline)) { return min(b * CH + pt * 16 + e * 8, last & -8); };
+    auto look_up = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) page[pt][e] = table[eight(b, pt, e) >> a.shift];
+    };
+    auto offset = [&](int b, int pt, int e) __attribute__((always_inline)) {
+        const int id = __builtin_amdgcn_readfirstlane(page[pt][e]);      // (or a lane's choice between two becomes an index into memory)
+        return ((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.page_stride + (eight(b, pt, e) & ((1 << a.shift) - 1)) * a.pos_stride;
+    };
+    auto load_keys = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) {
+            const long long lo = offset(b, pt, 0), hi = offset(b, pt, 1);
+            const int in8 = min(n16 & 7, last - (n16 & 8 ? eight(b, pt, 1) : eight(b, pt, 0)));
+            const bf16_t *kp = kb + (n16 & 8 ? hi : lo) + in8 * a.pos_stride + kg * 8;
+#pragma unroll
+            for (int ks = 0; ks < QS; ++ks) kf[pt][ks] = *reinterpret_cast<const u32x4_t *>(kp + ks * 32);
+        }
+    };
+    auto load_values = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) {
+            const long long lo = offset(b, pt, 0), hi = offset(b, pt, 1);
+            const int rest = last - (kg & 2 ? eight(b, pt, 1) : eight(b, pt, 0));
+            const bf16_t *vp = vb + (kg & 2 ? hi : lo) + n16 * DT;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vr[pt][i] = *reinterpret_cast<const vword *>(vp + min((kg & 1) * 4 + i, rest) * a.pos_stride);
+        }
+    };
+    auto enter = [&]() __attribute__((always_inline)) {
+        while (unit - before >= (long long)f.blocks * f.pair_groups * a.Hkv && r + 1 < a.n_requests) {   // on to the next request with units
             before += (long long)f.blocks * f.pair_groups * a.Hkv;
-            if (++r >= a.n_requests) return;                  // (never: the units lie in some request)
-            f = battn_few_shape(a, r, PAIRS, CH);
+            f = battn_few_shape(a, ++r, PAIRS, CH);
         }
         const long long in = unit - before;
-        const int group = (int)(in / f.blocks), b0 = (int)(in - (long long)group * f.blocks);
-        const int kvh = group / f.pair_groups, pg = group - kvh * f.pair_groups;
-        const int b1 = (int)min((long long)f.blocks, b0 + (unit_end - unit));
-        const int r0 = max(a.row_start[r], 0), n = f.n, len = battn_len(a, r), base = len - n, last = len - 1;
-        const int pairs = min(PAIRS, n * a.group - pg * PAIRS);                  // (n * group: at most the rows and heads of a call)
-
-        // the group's queries
-        __syncthreads();
-        for (int i = tid; i < PAIRS * (HD / 8); i += 256) {
-            const int p = i / (HD / 8), d = (i % (HD / 8)) * 8, pair = pg * PAIRS + min(p, pairs - 1);
+        const int group = (int)battn_divide(in, f.blocks);
+        b0 = (int)(in - (long long)group * f.blocks);
+        b1 = (int)min((long long)f.blocks, b0 + (unit_end - unit));
+        kvh = group / f.pair_groups;
+        pg = group - kvh * f.pair_groups;
+        r0 = max(a.row_start[r], 0);
+        len = battn_len(a, r);
+        last = len - 1;
+        pairs = min(PAIRS, f.n * a.group - pg * PAIRS);       // (rows times heads: at most those of a call)
+        // wavefronts that share a block, 16 NT pairs each; a wavefront's pairs; its blocks: wb, wb + step, ...
+        const int pw = PW == 1 || pairs <= 16 * NT ? 1 : PW;
+        wp = wave & (pw - 1); wb = wave / pw; step = 4 / pw; wave_pair = wp * 16 * NT;
+        table = (const_ints)(uintptr_t)(a.table + (size_t)r * a.width);
+        kb = (const bf16_t *)a.k + kvh * a.head_stride;
+        vb = (const bf16_t *)a.v + kvh * a.head_stride;
+        any = len > 0 && wave_pair < pairs && b0 + wb < b1;
+        if (any) look_up(b0 + wb);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            const int p = (i * 256 + tid) / (HD / 8), d = (tid % (HD / 8)) * 8, pair = pg * PAIRS + min(p, pairs - 1);
             const long long at = (long long)(r0 + pair / a.group) * a.q_stride + (kvh * a.group + pair % a.group) * HD + d;
             if constexpr (NP == 1) {
-                *reinterpret_cast<u32x4_t *>(ql + p * QROW + d) = *reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + at) ^ (flip | flip >> 16);
+                qv[i][0] = *reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + at);
+            } else {
+                qv[i][0] = *reinterpret_cast<const u32x4_t *>((const float *)a.q + at);
+                qv[i][1] = *reinterpret_cast<const u32x4_t *>((const float *)a.q + at + 4);
+            }
+        }
+        if (any) {
+            load_keys(b0 + wb);
+            load_values(b0 + wb);
+            look_up(b0 + wb + step);
+        }
+    };
+    enter();
+    while (true) {
+        const int base = len - f.n, pw = 4 / step;
+        __syncthreads();                                      // nobody reads the last group's queries any more
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            if (PAIRS * (HD / 8) < 256 && tid >= PAIRS * (HD / 8)) break;
+            bf16_t *to = ql + ((i * 256 + tid) / (HD / 8)) * QROW + (tid % (HD / 8)) * 8;
+            if constexpr (NP == 1) {
+                *reinterpret_cast<u32x4_t *>(to) = qv[i][0] ^ (flip | flip >> 16);
             } else {
                 float v[8];
                 bf16x8_t planes[3];
-                Piece<float>::load((const float *)a.q + at, v);
-                Piece<float>::load((const float *)a.q + at + 4, v + 4);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(__float_as_uint(v[e]) ^ flip);
+                for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(qv[i][e >> 2][e & 3] ^ flip);
                 battn_planes<3>(v, planes);
 #pragma unroll
-                for (int q = 0; q < 3; ++q) *reinterpret_cast<bf16x8_t *>(ql + (q * PAIRS + p) * QROW + d) = planes[q];
+                for (int x = 0; x < 3; ++x) *reinterpret_cast<bf16x8_t *>(to + x * PAIRS * QROW) = planes[x];
             }
         }
         __syncthreads();
@@ -525,52 +599,6 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
             for (int d = 0; d < DT; ++d) o[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
         const int first_limit = base + pg * PAIRS / a.group;
-        const const_ints table = (const_ints)(uintptr_t)(a.table + (size_t)r * a.width);
-        const bf16_t *kb = (const bf16_t *)a.k + kvh * a.head_stride, *vb = (const bf16_t *)a.v + kvh * a.head_stride;
-        // A block's keys and values are requested while the block before it is worked on, its pages one block earlier still.
-        u32x4_t kf[PT][QS];                                   // position 16 pt + n16, dimensions 32 ks + 8 kg ...
-        vword vr[PT][4];                                      // position 16 pt + 4 kg + i, dimensions DT n16 ...
-        int page[PT][2];
-        // first position of the block's e-th eight of tile pt (a page holds at least eight); positions past the last one repeat it
-        auto eight = [&](int b, int pt, int e) __attribute__((always_inline)) { return min(b * CH + pt * 16 + e * 8, last & -8); };
-        auto look_up = [&](int b) __attribute__((always_inline)) {
-#pragma unroll
-            for (int pt = 0; pt < PT; ++pt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) page[pt][e] = table[eight(b, pt, e) >> a.shift];
-        };
-        auto offset = [&](int b, int pt, int e) __attribute__((always_inline)) {
-            const int id = __builtin_amdgcn_readfirstlane(page[pt][e]);      // (or a lane's choice between two becomes an index into memory)
-            return ((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.page_stride + (eight(b, pt, e) & ((1 << a.shift) - 1)) * a.pos_stride;
-        };
-        auto load_keys = [&](int b) __attribute__((always_inline)) {
-#pragma unroll
-            for (int pt = 0; pt < PT; ++pt) {
-                const long long lo = offset(b, pt, 0), hi = offset(b, pt, 1);
-                const int in8 = min(n16 & 7, last - (n16 & 8 ? eight(b, pt, 1) : eight(b, pt, 0)));
-                const bf16_t *kp = kb + (n16 & 8 ? hi : lo) + in8 * a.pos_stride + kg * 8;
-#pragma unroll
-                for (int ks = 0; ks < QS; ++ks) kf[pt][ks] = *reinterpret_cast<const u32x4_t *>(kp + ks * 32);
-            }
-        };
-        auto load_values = [&](int b) __attribute__((always_inline)) {
-#pragma unroll
-            for (int pt = 0; pt < PT; ++pt) {
-                const long long lo = offset(b, pt, 0), hi = offset(b, pt, 1);
-                const int rest = last - (kg & 2 ? eight(b, pt, 1) : eight(b, pt, 0));
-                const bf16_t *vp = vb + (kg & 2 ? hi : lo) + n16 * DT;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) vr[pt][i] = *reinterpret_cast<const vword *>(vp + min((kg & 1) * 4 + i, rest) * a.pos_stride);
-            }
-        };
-        constexpr int STEP = 4 / PW;
-        const bool any = len > 0 && wave_pair < pairs && b0 + wb < b1;
-        if (any) {
-            look_up(b0 + wb);
-            load_keys(b0 + wb);
-            load_values(b0 + wb);
-            look_up(b0 + wb + STEP);
-        }
         // (two builds, with a next block and without: what is in flight where a value is waited for has to be known)
         auto work = [&](int b, auto more_) __attribute__((always_inline)) {
             constexpr bool more = decltype(more_)::value;
@@ -594,7 +622,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
                     }
             }
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (more) load_keys(b + STEP);
+            if constexpr (more) load_keys(b + step);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -645,8 +673,8 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d) asm volatile("" : "+v"(vf[hf][d]));       // all of it here: the next values go to the same registers
             if constexpr (more) {
-                load_values(b + STEP);
-                look_up(b + 2 * STEP);
+                load_values(b + step);
+                look_up(b + 2 * step);
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -666,13 +694,19 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
         };
         if (any) {
             int b = b0 + wb;
-            for (; b + STEP < b1; b += STEP) work(b, std::true_type{});
+            for (; b + step < b1; b += step) work(b, std::true_type{});
             work(b, std::false_type{});
         }
 
+        // the run goes on: the next group's loads are on their way while this one is finished
+        const bool whole = b0 == 0 && b1 == f.blocks, begins = b0 == 0, goes_on = unit + (b1 - b0) < unit_end;
+        const int this_pairs = pairs, this_r0 = r0, this_kvh = kvh, this_pair = pg * PAIRS;
+        const long long group_end = unit - b0 + f.blocks - 1;     // the group's last unit
+        unit += b1 - b0;
+        if (goes_on) enter();
+
         // the wavefronts' shares of each tile: thread (pair, dimensions) adds them up and writes them out, or leaves them for the merge
-        const bool whole = b0 == 0 && b1 == f.blocks;
-        float *slot = slots + (size_t)(2 * w + (b0 == 0)) * battn_few_slot<HD>(PAIRS);
+        float *slot = slots + (size_t)(2 * w + begins) * battn_few_slot<HD>(PAIRS);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             l[t] += lane_xor(l[t], 16);
@@ -687,23 +721,21 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
             __syncthreads();
             constexpr int V = HD * PW / 16, TP = HD / V;      // values per thread, threads per pair
             const int q16 = tid / TP, p = (q16 >> 4) * 16 * NT + t * 16 + (q16 & 15), d0 = (tid % TP) * V;
-            const float *share = mb + ((q16 >> 4) * 16 + (q16 & 15)) * MROW;         // of the first of the wavefronts that have this pair
+            const float *share = mb + (((q16 >> 4) & (pw - 1)) * 16 + (q16 & 15)) * MROW;         // of the first of the wavefronts that have this pair
             float top = -INFINITY, sum = 0.f, v[V];
-#pragma unroll
-            for (int x = 0; x < 4; x += PW) top = fmaxf(top, share[x * 16 * MROW + HD]);
+            for (int x = 0; x < 4; x += pw) top = fmaxf(top, share[x * 16 * MROW + HD]);
 #pragma unroll
             for (int e = 0; e < V; ++e) v[e] = 0.f;
-#pragma unroll
-            for (int x = 0; x < 4; x += PW) {
+            for (int x = 0; x < 4; x += pw) {
                 const float *m = share + x * 16 * MROW;
                 const float k = m[HD] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[HD] - top);
                 sum = fmaf(m[HD + 1], k, sum);
 #pragma unroll
                 for (int e = 0; e < V; ++e) v[e] = fmaf(m[d0 + e], k, v[e]);
             }
-            if (p < pairs) {
+            if (p < this_pairs && q16 < 16 * pw) {
                 if (whole) {
-                    battn_few_out<V, HD, NP>(a, r0, kvh, pg * PAIRS + p, d0, v, sum);
+                    battn_few_out<V, HD, NP>(a, this_r0, this_kvh, this_pair + p, d0, v, sum);
                 } else {
                     float *to = slot + p * MROW;
                     store_values<V>(to + d0, v);
@@ -712,73 +744,77 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
             }
             __syncthreads();
         }
-        if (!whole && b0 == 0 && tid == 0) {
-            const long long g0 = unit;                        // the group's first unit: it goes on in the runs behind this one
-            merges[w] = FewMerge{run_of(g0 + f.blocks - 1) - w + 1, r0, kvh, pg * PAIRS, pairs};
-        }
-        unit += b1 - b0;
+        if (!whole && begins && tid == 0)                     // it goes on in the runs behind this one
+            merges[w] = FewMerge{battn_run_of(group_end, q, rem) - w + 1, this_r0, this_kvh, this_pair, this_pairs};
+        if (!goes_on) return;
     }
 }
 
-// Joins the partial results of a group: four wavefronts a pair, a quarter of the runs each (every fourth), four requested at a time. In a launch of its own: the last
-// workgroup of a group doing it inside the first launch had to fetch up to 32 runs' results of all pairs by itself, one memory
-// latency after the other (two requests at 100 000 positions: 286 us).
-constexpr int BM_NT = 1024, BM_PAIRS = 4;
+// Joins the partial results of a group. HD/4 lanes have a pair, four values each, and take its runs' results one after the other, four requested at a
+// time; where the group lies in more than four runs, four such teams share them. In a launch of its own: the last workgroup of a group doing it inside
+// the first launch had to fetch up to 32 runs' results of all pairs by itself, one memory latency after the other (two requests at
+// 100 000 positions: 286 us in all, 168 us in two launches).
+constexpr int BM_NT = 256;
+template <int HD> __host__ __device__ constexpr int battn_merge_teams() { return BM_NT * 4 / HD; }
 template <int HD, int NP>
 __global__ __launch_bounds__(BM_NT) void battn_merge_kernel(BattnArgs a, int slot_pairs) {
-    constexpr int V = HD / 64, MROW = HD + BF_PAD, U = 4;
-    __shared__ float part[BM_NT / 64][HD + 2];
+    constexpr int LP = HD / 4, TEAMS = battn_merge_teams<HD>(), MROW = HD + BF_PAD, U = 4;
+    __shared__ f32x4_t part[TEAMS][LP];
+    __shared__ float part_top[TEAMS], part_sum[TEAMS];
     const FewMerge m = ((const FewMerge *)a.ws)[blockIdx.x];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = wave & 3;
     if (m.runs == 0) return;                                  // the whole workgroup
+    const int lane = threadIdx.x % LP, team = threadIdx.x / LP;
+    const int subs = m.runs > 4 ? 4 : 1, sub = team & (subs - 1), at_once = TEAMS / subs;
     const size_t slot = battn_few_slot<HD>(slot_pairs);
-    for (int p0 = blockIdx.y * BM_PAIRS; p0 < m.pairs; p0 += gridDim.y * BM_PAIRS) {
-        const int p = p0 + (wave >> 2);
+    for (int p0 = blockIdx.y * at_once; p0 < m.pairs; p0 += gridDim.y * at_once) {
+        const int p = p0 + team / subs;
         // run x's partial result is its second one (a group that begins there) for the first run, its first one for the others
         const float *first = (const float *)((const char *)a.ws + battn_few_merges()) + 2 * blockIdx.x * slot + min(p, m.pairs - 1) * MROW;
-        float top = -INFINITY, sum = 0.f, v[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = 0.f;
-        for (int x = sub; x < m.runs; x += 4 * U) {
-            float at[U], l[U], w[U][V];
+        float top = -INFINITY, sum = 0.f;
+        f32x4_t v{0.f, 0.f, 0.f, 0.f};
+        for (int x = sub; x < m.runs; x += subs * U) {
+            float at[U], l[U];
+            f32x4_t w[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int y = min(x + 4 * u, m.runs - 1);
-                const float *from = first + (2 * y + (y == 0)) * slot;
-                at[u] = from[HD];
-                l[u] = from[HD + 1];
-#pragma unroll
-                for (int e = 0; e < V; ++e) w[u][e] = from[lane * V + e];
+                const int y = x + subs * u;
+                at[u] = -INFINITY;
+                if (y < m.runs) {
+                    const float *from = first + (2 * y + (y == 0)) * slot;
+                    at[u] = from[HD];
+                    l[u] = from[HD + 1];
+                    w[u] = *reinterpret_cast<const f32x4_t *>(from + lane * 4);
+                }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (x + 4 * u >= m.runs || at[u] == -INFINITY) continue;
+                if (at[u] == -INFINITY) continue;
                 const float now = fmaxf(top, at[u]), k0 = __builtin_amdgcn_exp2f(top - now), k1 = __builtin_amdgcn_exp2f(at[u] - now);
                 top = now;
                 sum = sum * k0 + l[u] * k1;
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[e] = v[e] * k0 + w[u][e] * k1;
+                v = v * k0 + w[u] * k1;
             }
         }
-#pragma unroll
-        for (int e = 0; e < V; ++e) part[wave][lane * V + e] = v[e];
-        if (lane == 0) { part[wave][HD] = top; part[wave][HD + 1] = sum; }
-        __syncthreads();
+        if (subs > 1) {
+            part[team][lane] = v;
+            if (lane == 0) { part_top[team] = top; part_sum[team] = sum; }
+            __syncthreads();
+            if (sub == 0) {
+                for (int x = 1; x < subs; ++x) top = fmaxf(top, part_top[team + x]);
+                sum = 0.f;
+                v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                for (int x = 0; x < subs; ++x) {
+                    const float k = part_top[team + x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part_top[team + x] - top);
+                    sum = fmaf(part_sum[team + x], k, sum);
+                    v += part[team + x][lane] * k;
+                }
+            }
+            __syncthreads();
+        }
         if (sub == 0 && p < m.pairs) {
-            top = fmaxf(fmaxf(part[wave][HD], part[wave + 1][HD]), fmaxf(part[wave + 2][HD], part[wave + 3][HD]));
-            sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = 0.f;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const float k = part[wave + x][HD] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part[wave + x][HD] - top);
-                sum = fmaf(part[wave + x][HD + 1], k, sum);
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[e] = fmaf(part[wave + x][lane * V + e], k, v[e]);
-            }
-            battn_few_out<V, HD, NP>(a, m.r0, m.kvh, m.pair + p, lane * V, v, sum);
+            float out[4] = {v[0], v[1], v[2], v[3]};
+            battn_few_out<4, HD, NP>(a, m.r0, m.kvh, m.pair + p, lane * 4, out, sum);
         }
-        __syncthreads();
     }
 }
 

@@ -96,8 +96,9 @@ static void launch_few(const BattnArgs &a, int64_t most, hipStream_t s) {
     const int64_t units = blocks < INT32_MAX ? blocks * groups * a.Hkv : INT64_MAX;      // at most
     const unsigned runs = (unsigned)(units / 4 + 1 < BF_WGS ? units / 4 + 1 : BF_WGS);
     hipLaunchKernelGGL((battn_few_kernel<HD, NT, PW, NP>), dim3(runs), dim3(256), (battn_few_lds<HD, NT, PW, NP>()), s, a);
-    const int pairs = (int)(most < 16 * NT * PW ? most : 16 * NT * PW);
-    hipLaunchKernelGGL((battn_merge_kernel<HD, NP>), dim3(runs, (pairs + BM_PAIRS - 1) / BM_PAIRS), dim3(BM_NT), 0, s, a, 16 * NT * PW);
+    // few groups lie in many runs each, whose pairs then take four teams of lanes
+    const int pairs = (int)(most < 16 * NT * PW ? most : 16 * NT * PW), at_once = groups * a.Hkv < BF_WGS / 4 ? battn_merge_teams<HD>() / 4 : battn_merge_teams<HD>();
+    hipLaunchKernelGGL((battn_merge_kernel<HD, NP>), dim3(runs, (pairs + at_once - 1) / at_once), dim3(BM_NT), 0, s, a, 16 * NT * PW);
 }
 
 // attention over a bf16 cache
