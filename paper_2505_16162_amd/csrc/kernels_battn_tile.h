@@ -1,0 +1,353 @@
+// Attention of a batch's many rows in bf16: over pages (PAGED) or over their own prompts' rows.
+#pragma once
+#include <climits>
+
+#include "battn_common.h"
+
+namespace ks {
+
+// ------------------------------------------------------------------------------------------
+// Many rows, bf16: tiles of 128 (row, head) pairs of one kv head, 32 per wavefront, on the matrix cores.
+// Everything is computed transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane keeps one pair from the scores to the output: the
+// accumulators of S^T (position 8(i/4) + 4(lane/32) + i%4 of pair lane%32 in register i) are, rounded and packed as they lie, the operand of the
+// second product, whose other operand takes the values' positions in the same order by transposing reads of LDS. Nothing is
+// exchanged between lanes but one maximum per block.
+// Keys and values come in blocks of 64 positions straight to LDS, one block ahead; 16-byte pieces of a row are stored in an order
+// (exclusive or with the row's number) in which neither the keys' reads (32 rows, two pieces each) nor the values' (4 rows, 32
+// bytes each) meet in a bank.
+// ------------------------------------------------------------------------------------------
+constexpr int BT_PAIRS = 128, BT_CH = 64;
+
+// Tile `index` of the batch: its request and its number in there; false behind the last. Every wavefront for itself, 64 requests at a time.
+__device__ __forceinline__ bool battn_find_tile(const BattnArgs &a, int index, int &r_out, int &tile_out, int &tiles_out) {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int r0 = 0; r0 < a.n_requests; r0 += 64) {
+        const int r = r0 + lane;
+        int mine = 0;
+        if (r < a.n_requests) {
+            const long long n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
+            if (n > a.few_rows) mine = (int)((n * a.group + BT_PAIRS - 1) / BT_PAIRS);
+        }
+        int upto = mine;
+        for (int off = 1; off < 64; off <<= 1) {
+            const int u = __shfl_up(upto, off);
+            if (lane >= off) upto += u;
+        }
+        const unsigned long long past = __ballot(index < before + upto);
+        if (past) {
+            const int src = __builtin_ctzll(past);
+            r_out = r0 + src;
+            tiles_out = __builtin_amdgcn_readlane(mine, src);
+            tile_out = index - before - (__builtin_amdgcn_readlane(upto, src) - tiles_out);
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+template <int HD> constexpr int battn_tile_lds() { return 2 * 2 * BT_CH * HD * 2; }
+
+// Over pages the batch's tiles are dealt to the workgroups in equal runs, as in battn_few_kernel, by their cost: a tile's is the positions before its request's
+// new rows and those of its own pairs, times the heads of a group (in a pair's rows counted exactly: base * group + the pairs up to its last). It is at most
+// what its blocks of 64 positions hold, so a run that begins x into a tile begins with block x / (64 group) of it, and a run of
+// 64 group or more is never empty. The costs before a tile have a closed form.
+struct TileShape {
+    int n, tiles;                       // rows (0: not this kernel's), tiles of a kv head
+    long long step, pairs;              // cost of a tile without its own pairs; all pairs
+    __device__ __forceinline__ long long before(int t) const { return t * step + (long long)(BT_PAIRS / 2) * t * (t + 1); }      // (t < tiles)
+    __device__ __forceinline__ long long total() const { return tiles ? before(tiles - 1) + step + pairs : 0; }
+};
+constexpr int BT_FAR = 1 << 24;         // positions beyond count as so many
+__device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r) {
+    TileShape f{0, 0, 0, 0};
+    const int n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
+    if (n > 0 && n > a.few_rows) {
+        f.n = n;
+        f.pairs = (long long)n * a.group;
+        f.tiles = (int)((f.pairs + BT_PAIRS - 1) / BT_PAIRS);
+        f.step = (long long)min(max(battn_len(a, r) - n, 0), BT_FAR) * a.group;
+    }
+    return f;
+}
+
+template <int HD, bool PAGED>
+__global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
+    constexpr int KS = HD / 16, DT = HD / 32, SL = HD / 8, RB = HD * 2, MROW = HD + BF_PAD;
+    constexpr int KV = BT_CH * RB;                            // bytes of a block's keys (or values)
+    constexpr int ROWS = 64 / SL, NI = KV / 1024 / 4;         // rows a wavefront's load covers, loads per wavefront for the keys
+    extern __shared__ __align__(16) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const unsigned int l0 = (unsigned int)(uintptr_t)BATTN_LDS(lds);
+    const float c2 = fabsf(a.scale2);
+    const unsigned int flip = a.scale2 < 0.f ? 0x80008000u : 0u;
+
+    int r = 0, kvh, tile;
+    TileShape f{0, 0, 0, 0};
+    // the run: where it is and where it ends, in cost; the cost before the tile
+    long long at = 0, end = 0, before = 0, run_q = 0, run_rem = 0;
+    int run = 0;
+    const long long block_cost = 64ll * a.group;
+    if constexpr (PAGED) {
+        // runs next to each other on one XCD (workgroups are dealt round the eight), where they share keys and values
+        run = (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3));
+        if (tid == 0) ((FewMerge *)a.ws)[run] = FewMerge{0, 0, 0, 0, 0};
+        long long total = 0;
+        for (int pass = 0; pass < 2; ++pass) {
+            bool found = false;
+            for (int q0 = 0; q0 < a.n_requests && !found; q0 += 64) {
+                long long upto = 0;
+                if (q0 + lane < a.n_requests) upto = battn_tile_shape(a, q0 + lane).total() * a.Hkv;
+                for (int off = 1; off < 64; off <<= 1) {
+                    const long long u = __shfl_up(upto, off);
+                    if (lane >= off) upto += u;
+                }
+                if (pass == 0) total += battn_lane(upto, 63);
+                if (pass == 0 && q0 + 64 >= a.n_requests) {   // the total is known
+                    if (total == 0) return;
+                    const int runs = (int)max(1ll, min((long long)gridDim.x, total / (2 * block_cost)));      // two blocks at least
+                    if (run >= runs) return;
+                    run_q = battn_divide(total, runs);
+                    run_rem = total - run_q * runs;
+                    at = run * run_q + min((long long)run, run_rem);
+                    end = (run + 1) * run_q + min((long long)run + 1, run_rem);
+                }
+                if (pass == 1 || a.n_requests <= 64) {
+                    const unsigned long long past = __ballot(at < before + upto);
+                    found = past != 0;
+                    if (found) {
+                        const int src = __builtin_ctzll(past);
+                        r = q0 + src;
+                        if (src > 0) before += battn_lane(upto, src - 1);
+                    } else {
+                        before += battn_lane(upto, 63);
+                    }
+                }
+            }
+            if (found) break;
+        }
+        f = battn_tile_shape(a, r);
+        kvh = (int)battn_divide(at - before, f.total());
+        before += kvh * f.total();
+        int lo = 0, hi = f.tiles;
+        while (hi - lo > 1) {                                 // the last tile that begins at or before `at`
+            const int mid = (lo + hi) >> 1;
+            if (before + f.before(mid) <= at) lo = mid;
+            else hi = mid;
+        }
+        tile = lo;
+        before += f.before(tile);
+    } else {
+        kvh = blockIdx.x % a.Hkv;                             // (a kv head's tiles run behind few L2s)
+        if (!battn_find_tile(a, blockIdx.x / a.Hkv, r, tile, f.tiles)) return;
+        tile = f.tiles - 1 - tile;                            // long ones first
+        f.n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
+        f.pairs = (long long)f.n * a.group;
+    }
+    int buf = 0;                                              // where the next block goes
+    // the segment: blocks [b0, b1) of a tile
+    int r0, n, len, last, base, b0, b1, n_blocks;
+    const bf16_t *kb, *vb;
+    const_ints table;
+    // first row of the wavefront's i-th load of block c (rows past the request's last repeat that one)
+    auto load_row = [&](int c, int i) __attribute__((always_inline)) { return min(c * BT_CH + (i * 4 + wave) * ROWS, last & -ROWS); };
+    const int kpiece = (lane % SL) ^ ((wave * ROWS + lane / SL) & (SL - 1)), vpiece = (lane % SL) ^ (((lane / SL) & 3) << 1);
+    int page[NI];
+    auto look_up = [&](int c) __attribute__((always_inline)) {                               // the pages of block c
+        if constexpr (PAGED)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) page[i] = table[load_row(c, i) >> a.shift];
+    };
+    auto issue = [&](int c, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int b = load_row(c, i), in = min(lane / SL, last - b);
+            const unsigned int d = l0 + buf * 2 * KV + (i * 4 + wave) * 1024;
+            if constexpr (PAGED) {
+                const int pg = (unsigned)page[i] < (unsigned)a.n_pages ? page[i] : 0;
+                const long long at = pg * a.page_stride + (b & ((1 << a.shift) - 1)) * a.pos_stride;
+                const unsigned int off = (unsigned int)in * (unsigned int)a.pos_stride * 2u;
+                battn_dma(kb + at, off + kpiece * 16, d);
+                battn_dma(vb + at, off + vpiece * 16, d + KV);
+            } else {
+                battn_dma(kb + b * a.k_stride, (unsigned int)in * (unsigned int)a.k_stride * 2u + kpiece * 16, d);
+                battn_dma(vb + b * a.v_stride, (unsigned int)in * (unsigned int)a.v_stride * 2u + vpiece * 16, d + KV);
+            }
+        }
+    };
+    const int k_at = col * RB, v_row = 4 * half + ((lane & 15) >> 2), v_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    auto enter = [&]() __attribute__((always_inline)) {       // the segment of `tile` that begins at `at`
+        r0 = max(a.row_start[r], 0);
+        n = f.n;
+        len = PAGED ? battn_len(a, r) : n;
+        last = len - 1;
+        base = len - n;                                       // position of the request's first new row
+        const int tile_last = (int)((min((long long)(tile + 1) * BT_PAIRS, f.pairs) - 1) / a.group);
+        n_blocks = (max(base, 0) + tile_last) / BT_CH + 1;
+        b0 = 0;
+        b1 = n_blocks;
+        kb = (const bf16_t *)a.k;
+        vb = (const bf16_t *)a.v;
+        if constexpr (PAGED) {
+            const long long cost = f.step + min((long long)(tile + 1) * BT_PAIRS, f.pairs);
+            b0 = (int)battn_divide(at - before, block_cost);
+            if (end < before + cost) b1 = (int)min((long long)n_blocks, battn_divide(end - before, block_cost));
+            kb += kvh * a.head_stride;
+            vb += kvh * a.head_stride;
+            table = (const_ints)(uintptr_t)(a.table + (size_t)r * a.width);
+        } else {
+            kb += (long long)r0 * a.k_stride + kvh * HD;
+            vb += (long long)r0 * a.v_stride + kvh * HD;
+        }
+        if (len > 0 && b0 < b1) {
+            look_up(b0);
+            issue(b0, buf);
+            look_up(b0 + 1);
+        }
+    };
+    enter();
+    while (b0 < b1) {
+        const long long p0 = (long long)tile * BT_PAIRS;
+        const int wave_first = (int)((p0 + wave * 32) / a.group);                                     // the wavefront's first row
+        const int wave_last = p0 + wave * 32 < f.pairs ? (int)((min(p0 + wave * 32 + 32, f.pairs) - 1) / a.group) : INT_MIN / 2;      // ... and last one
+        const long long pair = min(p0 + wave * 32 + col, f.pairs - 1);
+        const bool live = p0 + wave * 32 + col < f.pairs;
+        const int row = (int)(pair / a.group), g = (int)(pair - (long long)row * a.group);
+        const int limit = base + row;                         // the lane's last visible position
+        bf16x8_t qf[KS];                                          // dimensions 16 ks + 8 half ... of the lane's pair
+        {
+            const bf16_t *qp = (const bf16_t *)a.q + (long long)(r0 + row) * a.q_stride + (kvh * a.group + g) * HD + half * 8;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(qp + ks * 16) ^ flip);
+        }
+        float m = -INFINITY, off = -INFINITY, l = 0.f;
+        f32x16_t o[DT];
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+        for (int c = b0; c < b1; ++c, buf ^= 1) {
+            if (len <= 0) continue;                               // (nothing to see; the same for all)
+            battn_wait<0>();
+            battn_meet();                                         // block c is here and nobody reads block c-1 any more
+            if (c + 1 < b1) {
+                issue(c + 1, buf ^ 1);
+                look_up(c + 2);
+            }
+            if (c * BT_CH > base + wave_last) continue;           // beyond all of the wavefront's rows
+            const char *kl = lds + buf * 2 * KV;
+            const unsigned int vl = l0 + buf * 2 * KV + KV;
+            f32x16_t s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(kl + t * 32 * RB + k_at + (((2 * ks + half) ^ (col & (SL - 1))) * 16)));
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s[t], 0, 0, 0);
+                }
+            }
+            const bool diagonal = c * BT_CH + BT_CH - 1 > base + wave_first;
+            if (diagonal) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (c * BT_CH + t * 32 + 8 * (i / 4) + 4 * half + i % 4 > limit) s[t][i] = -INFINITY;
+            }
+            float cm = s[0][0];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) cm = fmaxf(cm, s[t][i]);
+            cm = fmaxf(cm, lane_xor(cm, 32));
+            m = fmaxf(m, cm);
+            const float off_new = m == -INFINITY ? 0.f : battn_rounded_product(m, c2), f = __builtin_amdgcn_exp2f(off - off_new);
+            off = off_new;
+            float ps = 0.f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], c2, -off));
+                    if (diagonal && c * BT_CH + t * 32 + 8 * (i / 4) + 4 * half + i % 4 > limit) s[t][i] = 0.f;      // (also where the scale is 0)
+                    ps += s[t][i];
+                }
+            l = l * f + ps;
+            if (__any(f != 1.0f)) {
+#pragma unroll
+                for (int t = 0; t < DT; ++t) o[t] *= f;
+            }
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {                      // 16 positions
+                const int t = st >> 1, i0 = (st & 1) * 8;
+                const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16(s[t][i0], s[t][i0 + 1]), pack_bf16(s[t][i0 + 2], s[t][i0 + 3]),
+                                                                         pack_bf16(s[t][i0 + 4], s[t][i0 + 5]), pack_bf16(s[t][i0 + 6], s[t][i0 + 7])});
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    // (rows st*16 + v_row and 8 on: the row's number ends in v_row & 3, whatever st)
+                    const unsigned int at = vl + (st * 16 + v_row) * RB + (((4 * dt + (v_col >> 3)) ^ ((v_row & 3) << 1)) * 16) + (v_col & 4) * 2;
+                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)at);
+                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)(at + 8 * RB));
+                    const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb, o[dt], 0, 0, 0);
+                }
+            }
+        }
+        l += lane_xor(l, 32);
+        const bool whole = b0 == 0 && b1 == n_blocks;
+        const int out_row = r0 + row, out_kvh = kvh;
+        bool goes_on = false;
+        if constexpr (PAGED) {
+            if (!whole && b0 == 0 && tid == 0)                // it goes on in the runs behind this one
+                ((FewMerge *)a.ws)[run] = FewMerge{battn_run_of(before + f.step + min((long long)(tile + 1) * BT_PAIRS, f.pairs) - 1, run_q, run_rem) - run + 1, r0, kvh,
+                                                   tile * BT_PAIRS, (int)min((long long)BT_PAIRS, f.pairs - p0)};
+        }
+        const int slot = 2 * run + (b0 == 0);
+        // on to the next tile: its first block is on its way while this one is written (the buffer that it goes to has been read by all)
+        if constexpr (PAGED) {
+            before += f.step + min((long long)(tile + 1) * BT_PAIRS, f.pairs);
+            goes_on = before < end;
+            if (goes_on) {
+                at = before;
+                if (++tile == f.tiles) {
+                    tile = 0;
+                    if (++kvh == a.Hkv) {
+                        kvh = 0;
+                        do {
+                            if (++r >= a.n_requests) goes_on = false;     // (never: the run lies in some requests)
+                            else f = battn_tile_shape(a, r);
+                        } while (goes_on && f.tiles == 0);
+                    }
+                }
+                if (goes_on) enter();
+            }
+        }
+        if (!live) {
+        } else if (!PAGED || whole) {
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            bf16_t *op = (bf16_t *)a.out + (long long)out_row * a.out_stride + (out_kvh * a.group + g) * HD + 4 * half;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const float v[4] = {o[t][4 * b] * inv, o[t][4 * b + 1] * inv, o[t][4 * b + 2] * inv, o[t][4 * b + 3] * inv};
+                    store_values<4>(op + t * 32 + b * 8, v);
+                }
+        } else {
+            float *to = (float *)((char *)a.ws + battn_few_merges()) + (size_t)slot * battn_few_slot<HD>(BT_PAIRS) + (wave * 32 + col) * MROW;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    *reinterpret_cast<f32x4_t *>(to + t * 32 + b * 8 + 4 * half) = f32x4_t{o[t][4 * b], o[t][4 * b + 1], o[t][4 * b + 2], o[t][4 * b + 3]};
+            if (half == 0) { to[HD] = m == -INFINITY ? -INFINITY : off; to[HD + 1] = l; }
+        }
+        if (!goes_on) return;
+    }
+}
+
+}  // namespace ks

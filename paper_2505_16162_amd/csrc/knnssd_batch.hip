@@ -5,7 +5,9 @@
 #include <cmath>
 
 #include "hip_try.h"
-#include "kernels_battn.h"
+#include "kernels_battn_few.h"
+#include "kernels_battn_row.h"
+#include "kernels_battn_tile.h"
 #include "kernels_pages.h"
 #include "pages_check.h"
 
@@ -80,10 +82,22 @@ static int32_t rows_check(const int32_t *row_start_dev, int32_t n_requests, cons
     return KNNSSD_OK;
 }
 
-template <int HD, bool PAGED>
-static void launch_tiles(const BattnArgs &a, hipStream_t s) {
-    const int64_t tiles = ((int64_t)a.n_rows * a.group + BT_PAIRS - 1) / BT_PAIRS + a.n_requests;       // (at most; what is too much ends at once)
-    hipLaunchKernelGGL((battn_tile_kernel<HD, PAGED>), dim3((unsigned)(tiles * a.Hkv)), dim3(256), battn_tile_lds<HD>(), s, a);
+template <int HD>
+static void launch_merge(const BattnArgs &a, bool fp32, unsigned runs, int pairs, int64_t groups, int slot_pairs, hipStream_t s) {
+    // few groups lie in many runs each, whose pairs then take four teams of lanes
+    const int at_once = groups < BF_WGS / 4 ? battn_merge_teams<HD>() / 4 : battn_merge_teams<HD>();
+    const dim3 grid(runs, (pairs + at_once - 1) / at_once);
+    if (fp32) hipLaunchKernelGGL((battn_merge_kernel<HD, 3>), grid, dim3(BM_NT), 0, s, a, slot_pairs);
+    else hipLaunchKernelGGL((battn_merge_kernel<HD, 1>), grid, dim3(BM_NT), 0, s, a, slot_pairs);
+}
+
+// tiles at most; what is too much ends at once
+static int64_t tiles_bound(const BattnArgs &a) { return (((int64_t)a.n_rows * a.group + BT_PAIRS - 1) / BT_PAIRS + a.n_requests) * a.Hkv; }
+
+template <int HD>
+static void launch_paged_tiles(const BattnArgs &a, hipStream_t s) {
+    hipLaunchKernelGGL((battn_tile_kernel<HD, true>), dim3(BF_WGS), dim3(256), battn_tile_lds<HD>(), s, a);
+    launch_merge<HD>(a, false, BF_WGS, BT_PAIRS, tiles_bound(a), BT_PAIRS, s);
 }
 
 // most (row, head) pairs of one kv head for which a request goes through battn_few_kernel where battn_tile_kernel is there too
@@ -96,9 +110,7 @@ static void launch_few(const BattnArgs &a, int64_t most, hipStream_t s) {
     const int64_t units = blocks < INT32_MAX ? blocks * groups * a.Hkv : INT64_MAX;      // at most
     const unsigned runs = (unsigned)(units / 4 + 1 < BF_WGS ? units / 4 + 1 : BF_WGS);
     hipLaunchKernelGGL((battn_few_kernel<HD, NT, PW, NP>), dim3(runs), dim3(256), (battn_few_lds<HD, NT, PW, NP>()), s, a);
-    // few groups lie in many runs each, whose pairs then take four teams of lanes
-    const int pairs = (int)(most < 16 * NT * PW ? most : 16 * NT * PW), at_once = groups * a.Hkv < BF_WGS / 4 ? battn_merge_teams<HD>() / 4 : battn_merge_teams<HD>();
-    hipLaunchKernelGGL((battn_merge_kernel<HD, NP>), dim3(runs, (pairs + at_once - 1) / at_once), dim3(BM_NT), 0, s, a, 16 * NT * PW);
+    launch_merge<HD>(a, NP == 3, runs, (int)(most < 16 * NT * PW ? most : 16 * NT * PW), groups * a.Hkv, 16 * NT * PW, s);
 }
 
 // attention over a bf16 cache
@@ -117,12 +129,15 @@ static void launch_paged_bf16(BattnArgs a, int32_t dtype, int32_t most_rows, hip
         else if (most <= 32) launch_few<HD, 2, 1, 1>(a, most, s);
         else launch_few<HD, 2, 2, 1>(a, most, s);
     }
-    if (most > FEW_PAIRS) launch_tiles<HD, true>(a, s);
+    if (most > FEW_PAIRS) launch_paged_tiles<HD>(a, s);
 }
 
 template <int HD, bool PAGED>
 static void launch_battn(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, int32_t most_rows, hipStream_t s) {
-    if (!PAGED && dtype == KNNSSD_BF16) return launch_tiles<HD, false>(a, s);
+    if (!PAGED && dtype == KNNSSD_BF16) {
+        hipLaunchKernelGGL((battn_tile_kernel<HD, false>), dim3((unsigned)tiles_bound(a)), dim3(256), battn_tile_lds<HD>(), s, a);
+        return;
+    }
     if (PAGED && kv_dtype == KNNSSD_BF16) return launch_paged_bf16<HD>(a, dtype, most_rows, s);
     const int64_t items = (int64_t)a.n_rows * a.H;
     hipLaunchKernelGGL((battn_row_kernel<HD, PAGED>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
@@ -132,7 +147,7 @@ extern "C" size_t knnssd_paged_attention_bytes(const knnssd_pages *p, int32_t n_
     if (pages_check(p) != KNNSSD_OK || !dtype_ok(dtype) || !types_go_together(dtype, p->kv_dtype)) return 0;
     if (n_heads < 1 || n_heads > 65535 || n_heads % p->n_kv_heads) return 0;
     if (p->kv_dtype == KNNSSD_FP32) return 256;
-    const size_t slot = p->head_dim == 128 ? battn_few_slot<128>(FEW_PAIRS) : battn_few_slot<64>(FEW_PAIRS);
+    const size_t slot = p->head_dim == 128 ? battn_few_slot<128>(BT_PAIRS) : battn_few_slot<64>(BT_PAIRS);
     return battn_few_merges() + 2 * BF_WGS * slot * sizeof(float);
 }
 
