@@ -1,5 +1,7 @@
 // Attention of a batch's few rows over pages in bf16.
 #pragma once
+#include <cfloat>
+
 #include "battn_common.h"
 
 namespace ks {
@@ -90,7 +92,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
         }
         if (found) break;
     }
-    const float c2 = fabsf(a.scale2);
+    const float c2 = fmaxf(fabsf(a.scale2), FLT_MIN);         // (a hidden score, -inf, has to stay that under a scale of 0)
     const unsigned int flip = a.scale2 < 0.f ? 0x80000000u : 0u;
 
     // Where the run is: a group, its blocks [b0, b1) of the run. What follows sets these for the blocks from `unit` on, and requests the group's
@@ -252,8 +254,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
                     for (int i = 0; i < 4; ++i) cm = fmaxf(cm, s[t][pt][i]);
                 cm = fmaxf(cm, lane_xor(cm, 16));
                 cm = fmaxf(cm, lane_xor(cm, 32));
-                // (-inf times a scale of 0 would be NaN)
-                const float off_new = cm == -INFINITY ? off[t] : fmaxf(off[t], battn_rounded_product(cm, c2)), ref = off_new == -INFINITY ? 0.f : off_new;
+                const float off_new = fmaxf(off[t], battn_rounded_product(cm, c2)), ref = off_new == -INFINITY ? 0.f : off_new;
                 const float fac = __builtin_amdgcn_exp2f(off[t] - ref);
                 off[t] = off_new;
                 float ps = 0.f;
@@ -262,7 +263,6 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         s[t][pt][i] = __builtin_amdgcn_exp2f(fmaf(s[t][pt][i], c2, -ref));
-                        if (diagonal && pos0 + pt * 16 + 4 * kg + i > limit[t]) s[t][pt][i] = 0.f;
                         ps += s[t][pt][i];
                     }
                 l[t] = l[t] * fac + ps;

@@ -1,5 +1,6 @@
 // Attention of a batch's many rows in bf16: over pages (PAGED) or over their own prompts' rows.
 #pragma once
+#include <cfloat>
 #include <climits>
 
 #include "battn_common.h"
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     const unsigned int l0 = (unsigned int)(uintptr_t)BATTN_LDS(lds);
-    const float c2 = fabsf(a.scale2);
+    const float c2 = fmaxf(fabsf(a.scale2), FLT_MIN);         // (a hidden score, -inf, has to stay that under a scale of 0)
     const unsigned int flip = a.scale2 < 0.f ? 0x80008000u : 0u;
 
     int r = 0, kvh, tile;
@@ -177,7 +178,16 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
             }
         }
     };
-    const int k_at = col * RB, v_row = 4 * half + ((lane & 15) >> 2), v_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    // where the lane reads in a block: keys of position col, dimensions 16 ks + 8 half ...; values of position 4 half + (lane % 16) / 4 (and 8 on), four
+    // dimensions from 32 dt + 16 (lane / 16 % 2) + 4 (lane % 4)
+    unsigned int k_at[KS], v_at[DT];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) k_at[ks] = l0 + col * RB + (((2 * ks + half) ^ (col & (SL - 1))) * 16);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+        const int v_row = 4 * half + ((lane & 15) >> 2), v_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+        v_at[dt] = l0 + KV + v_row * RB + (((4 * dt + (v_col >> 3)) ^ ((v_row & 3) << 1)) * 16) + (v_col & 4) * 2;
+    }
     auto enter = [&]() __attribute__((always_inline)) {       // the segment of `tile` that begins at `at`
         r0 = max(a.row_start[r], 0);
         n = f.n;
@@ -222,36 +232,38 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(qp + ks * 16) ^ flip);
         }
-        float m = -INFINITY, off = -INFINITY, l = 0.f;
+        float ref = -INFINITY, l = 0.f;
         f32x16_t o[DT];
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
         for (int c = b0; c < b1; ++c, buf ^= 1) {
-            if (len <= 0) continue;                               // (nothing to see; the same for all)
+            if (len <= 0) continue;                           // (nothing to see; the same for all)
             battn_wait<0>();
-            battn_meet();                                         // block c is here and nobody reads block c-1 any more
+            battn_meet();                                     // block c is here and nobody reads block c-1 any more
             if (c + 1 < b1) {
                 issue(c + 1, buf ^ 1);
                 look_up(c + 2);
             }
-            if (c * BT_CH > base + wave_last) continue;           // beyond all of the wavefront's rows
-            const char *kl = lds + buf * 2 * KV;
-            const unsigned int vl = l0 + buf * 2 * KV + KV;
+            if (c * BT_CH > base + wave_last) continue;       // beyond all of the wavefront's rows
+            const unsigned int bl = buf * 2 * KV;
             f32x16_t s[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(kl + t * 32 * RB + k_at + (((2 * ks + half) ^ (col & (SL - 1))) * 16)));
+            for (int ks = 0; ks < KS; ++ks) {
+                unsigned int from = k_at[ks] + bl;
+                asm("" : "+v"(from));                         // (one address, the tiles by the read's own offset)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(__attribute__((address_space(3))) const u32x4_t *)(uintptr_t)(from + t * 32 * RB));
                     s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s[t], 0, 0, 0);
                 }
             }
-            const bool diagonal = c * BT_CH + BT_CH - 1 > base + wave_first;
-            if (diagonal) {
+            if (c * BT_CH + BT_CH - 1 > base + wave_first) {  // some of the block's positions lie behind some of the wavefront's rows
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -264,34 +276,42 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) cm = fmaxf(cm, s[t][i]);
             cm = fmaxf(cm, lane_xor(cm, 32));
-            m = fmaxf(m, cm);
-            const float off_new = m == -INFINITY ? 0.f : battn_rounded_product(m, c2), f = __builtin_amdgcn_exp2f(off - off_new);
-            off = off_new;
+            // The reference that the weights are taken against follows the largest score only where that has left it 2^8 behind, and then for all lanes:
+            // weights of up to 2^8 lose nothing (bf16 and fp32 have the same steps there), and what has been summed up is rescaled a few
+            // times in all, instead of in every block in which one of 32 pairs has a new largest score.
+            const float top = battn_rounded_product(cm, c2);
+            if (__builtin_expect(__any(top > ref + 8.f), 0)) {
+                const float now = fmaxf(ref, top), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
+                ref = now;
+                l *= f;
+#pragma unroll
+                for (int t = 0; t < DT; ++t) o[t] *= f;
+            }
+            const float off = ref == -INFINITY ? 0.f : ref;
             float ps = 0.f;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], c2, -off));
-                    if (diagonal && c * BT_CH + t * 32 + 8 * (i / 4) + 4 * half + i % 4 > limit) s[t][i] = 0.f;      // (also where the scale is 0)
                     ps += s[t][i];
                 }
-            l = l * f + ps;
-            if (__any(f != 1.0f)) {
+            l += ps;
+            unsigned int from[DT];
 #pragma unroll
-                for (int t = 0; t < DT; ++t) o[t] *= f;
+            for (int dt = 0; dt < DT; ++dt) {
+                from[dt] = v_at[dt] + bl;
+                asm("" : "+v"(from[dt]));
             }
 #pragma unroll
-            for (int st = 0; st < 4; ++st) {                      // 16 positions
+            for (int st = 0; st < 4; ++st) {                  // 16 positions
                 const int t = st >> 1, i0 = (st & 1) * 8;
                 const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16(s[t][i0], s[t][i0 + 1]), pack_bf16(s[t][i0 + 2], s[t][i0 + 3]),
                                                                          pack_bf16(s[t][i0 + 4], s[t][i0 + 5]), pack_bf16(s[t][i0 + 6], s[t][i0 + 7])});
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
-                    // (rows st*16 + v_row and 8 on: the row's number ends in v_row & 3, whatever st)
-                    const unsigned int at = vl + (st * 16 + v_row) * RB + (((4 * dt + (v_col >> 3)) ^ ((v_row & 3) << 1)) * 16) + (v_col & 4) * 2;
-                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)at);
-                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)(at + 8 * RB));
+                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)(from[dt] + st * 16 * RB));
+                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)(from[dt] + st * 16 * RB + 8 * RB));
                     const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
                     o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb, o[dt], 0, 0, 0);
                 }
@@ -344,7 +364,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
                     *reinterpret_cast<f32x4_t *>(to + t * 32 + b * 8 + 4 * half) = f32x4_t{o[t][4 * b], o[t][4 * b + 1], o[t][4 * b + 2], o[t][4 * b + 3]};
-            if (half == 0) { to[HD] = m == -INFINITY ? -INFINITY : off; to[HD + 1] = l; }
+            if (half == 0) { to[HD] = ref; to[HD + 1] = l; }
         }
         if (!goes_on) return;
     }
