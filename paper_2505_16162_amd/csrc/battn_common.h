@@ -6,13 +6,16 @@
 
 namespace ks {
 
+// ints that nothing writes while the kernel runs, by scalar loads where the index is the same for all lanes
+typedef const __attribute__((address_space(4))) int *const_ints;
+
 struct BattnArgs {
     const void *q, *k, *v;
     void *out;
     long long q_stride, out_stride;             // rows of q and out
     long long k_stride, v_stride;               // rows of k and v (prompts)
     long long page_stride, head_stride, pos_stride;
-    const int *table, *row_start, *kv_len;      // (kv_len, table: pages)
+    const_ints table, row_start, kv_len;        // (kv_len, table: pages)
     int n_requests, n_rows, width, shift, n_pages;
     int H, Hkv, group;
     float scale2;                               // scale * log2(e): softmax in powers of two
@@ -21,7 +24,7 @@ struct BattnArgs {
 };
 
 // request of row t < row_start[n], by bisection
-__device__ __forceinline__ int battn_request(const int *row_start, int n, int t) {
+__device__ __forceinline__ int battn_request(const_ints row_start, int n, int t) {
     int lo = 0, hi = n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -47,17 +50,20 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 #define BATTN_LDS(p) ((__attribute__((address_space(3))) char *)(p))
-typedef const __attribute__((address_space(4))) int *const_ints;        // read by scalar loads
 
 // lane i's value, known to be the same everywhere (scalar registers, scalar loads)
 __device__ __forceinline__ long long battn_lane(long long v, int i) {
     return (long long)(unsigned int)__builtin_amdgcn_readlane((int)v, i) | (long long)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32;
 }
 
+// the same for a value that the compiler has worked out in vector registers (64-bit comparisons and choices, conversions) though it is the same for all
+__device__ __forceinline__ int battn_same(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ long long battn_same(long long v) { return battn_lane(v, 0); }
+
 // 64 lanes' 16 bytes from base + off (bytes) to LDS, lane by lane behind lds_off. Not counted by the compiler: battn_wait. (s_nop: a
 // base that the vector unit has just written may be read five states later.)
 __device__ __forceinline__ void battn_dma(const void *base, unsigned int off, unsigned int lds_off) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(battn_lane((long long)(uintptr_t)base, 0)), "s"(__builtin_amdgcn_readfirstlane(lds_off)) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(battn_same((long long)(uintptr_t)base)), "s"(battn_same((int)lds_off)) : "memory");
 }
 template <int KEEP> __device__ __forceinline__ void battn_wait() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(KEEP) : "memory"); }
 // a workgroup's meeting that leaves loads in flight (this wavefront's LDS reads have returned)
@@ -107,12 +113,12 @@ __device__ __forceinline__ void battn_planes(const float *v, bf16x8_t *out) {
     }
 }
 
-// x / d for 0 <= x < 2^53 and d > 0: many times shorter than a division of 64-bit integers
+// x / d for 0 <= x < 2^53 and d > 0, the same for all lanes: many times shorter than a division of 64-bit integers
 __device__ __forceinline__ long long battn_divide(long long x, long long d) {
     long long q = (long long)((double)x / (double)d);
     if (q * d > x) --q;
     if ((q + 1) * d <= x) ++q;
-    return q;
+    return battn_same(q);
 }
 
 // run that has a unit, where the first rem runs have q + 1 units and the others q

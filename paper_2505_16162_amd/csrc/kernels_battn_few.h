@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
     int r = 0, runs = 0;
     const int w = blockIdx.x;
     if (tid == 0) merges[w] = FewMerge{0, 0, 0, 0, 0};
-    auto run_start = [&](int i) { return i * q + min((long long)i, rem); };      // rem runs of q + 1 units, the others of q
+    auto run_start = [&](int i) { return battn_same(i * q + min((long long)i, rem)); };      // rem runs of q + 1 units, the others of q
     for (int pass = 0; pass < 2; ++pass) {
         bool found = false;
         for (int r0 = 0; r0 < a.n_requests && !found; r0 += 64) {
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
             }
             if (pass == 0) total += battn_lane(upto, 63);
             if (pass == 0 && r0 + 64 >= a.n_requests) {       // the total is known
-                runs = (int)min((long long)gridDim.x, (total + 3) / 4);         // four units at least: a block for every wavefront
+                runs = battn_same((int)min((long long)gridDim.x, (total + 3) / 4));         // four units at least: a block for every wavefront
                 if (w >= runs) return;
                 q = battn_divide(total, runs);
                 rem = total - q * runs;
@@ -147,17 +147,17 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
         const long long in = unit - before;
         const int group = (int)battn_divide(in, f.blocks);
         b0 = (int)(in - (long long)group * f.blocks);
-        b1 = (int)min((long long)f.blocks, b0 + (unit_end - unit));
+        b1 = battn_same((int)min((long long)f.blocks, b0 + (unit_end - unit)));
         kvh = group / f.pair_groups;
         pg = group - kvh * f.pair_groups;
         r0 = max(a.row_start[r], 0);
-        len = battn_len(a, r);
+        len = battn_same(battn_len(a, r));
         last = len - 1;
         pairs = min(PAIRS, f.n * a.group - pg * PAIRS);       // (rows times heads: at most those of a call)
         // wavefronts that share a block, 16 NT pairs each; a wavefront's pairs; its blocks: wb, wb + step, ...
         const int pw = PW == 1 || pairs <= 16 * NT ? 1 : PW;
         wp = wave & (pw - 1); wb = wave / pw; step = 4 / pw; wave_pair = wp * 16 * NT;
-        table = (const_ints)(uintptr_t)(a.table + (size_t)r * a.width);
+        table = a.table + (size_t)r * a.width;
         kb = (const bf16_t *)a.k + kvh * a.head_stride;
         vb = (const bf16_t *)a.v + kvh * a.head_stride;
         any = len > 0 && wave_pair < pairs && b0 + wb < b1;
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
             const int pos0 = b * CH;
             const bool diagonal = pos0 + CH - 1 > first_limit;
             f32x4_t s[NT][PT];
-            const bf16_t *qb = ql + (wave_pair + n16) * QROW + kg * 8;
+            unsigned int qb = (unsigned int)(uintptr_t)BATTN_LDS(lds) + ((wave_pair + n16) * QROW + kg * 8) * 2;
             if (NT * NP > 1) asm volatile("" : "+v"(qb));     // (they are read again for every block: there is no room to keep them all)
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
                 for (int q = NP - 1; q >= 0; --q)
 #pragma unroll
                     for (int ks = 0; ks < QS; ++ks) {
-                        const bf16x8_t qf = *reinterpret_cast<const bf16x8_t *>(qb + (q * PAIRS + t * 16) * QROW + ks * 32);
+                        const bf16x8_t qf = *(__attribute__((address_space(3))) const bf16x8_t *)(uintptr_t)(qb + ((q * PAIRS + t * 16) * QROW + ks * 32) * 2);
 #pragma unroll
                         for (int pt = 0; pt < PT; ++pt) s[t][pt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[pt][ks]), qf, s[t][pt], 0, 0, 0);
                     }

@@ -108,12 +108,12 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
                 if (pass == 0) total += battn_lane(upto, 63);
                 if (pass == 0 && q0 + 64 >= a.n_requests) {   // the total is known
                     if (total == 0) return;
-                    const int runs = (int)max(1ll, min((long long)gridDim.x, total / (2 * block_cost)));      // two blocks at least
+                    const int runs = battn_same((int)max(1ll, min((long long)gridDim.x, battn_divide(total, 2 * block_cost))));      // two blocks at least
                     if (run >= runs) return;
                     run_q = battn_divide(total, runs);
                     run_rem = total - run_q * runs;
-                    at = run * run_q + min((long long)run, run_rem);
-                    end = (run + 1) * run_q + min((long long)run + 1, run_rem);
+                    at = battn_same(run * run_q + min((long long)run, run_rem));
+                    end = battn_same((run + 1) * run_q + min((long long)run + 1, run_rem));
                 }
                 if (pass == 1 || a.n_requests <= 64) {
                     const unsigned long long past = __ballot(at < before + upto);
@@ -190,11 +190,11 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
     }
     auto enter = [&]() __attribute__((always_inline)) {       // the segment of `tile` that begins at `at`
         r0 = max(a.row_start[r], 0);
-        n = f.n;
-        len = PAGED ? battn_len(a, r) : n;
+        n = battn_same(f.n);
+        len = PAGED ? battn_same(battn_len(a, r)) : n;
         last = len - 1;
         base = len - n;                                       // position of the request's first new row
-        const int tile_last = (int)((min((long long)(tile + 1) * BT_PAIRS, f.pairs) - 1) / a.group);
+        const int tile_last = battn_same((int)((min((long long)(tile + 1) * BT_PAIRS, f.pairs) - 1) / a.group));
         n_blocks = (max(base, 0) + tile_last) / BT_CH + 1;
         b0 = 0;
         b1 = n_blocks;
@@ -204,9 +204,10 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
             const long long cost = f.step + min((long long)(tile + 1) * BT_PAIRS, f.pairs);
             b0 = (int)battn_divide(at - before, block_cost);
             if (end < before + cost) b1 = (int)min((long long)n_blocks, battn_divide(end - before, block_cost));
+            b1 = battn_same(b1);
             kb += kvh * a.head_stride;
             vb += kvh * a.head_stride;
-            table = (const_ints)(uintptr_t)(a.table + (size_t)r * a.width);
+            table = a.table + (size_t)r * a.width;
         } else {
             kb += (long long)r0 * a.k_stride + kvh * HD;
             vb += (long long)r0 * a.v_stride + kvh * HD;
@@ -220,8 +221,8 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
     enter();
     while (b0 < b1) {
         const long long p0 = (long long)tile * BT_PAIRS;
-        const int wave_first = (int)((p0 + wave * 32) / a.group);                                     // the wavefront's first row
-        const int wave_last = p0 + wave * 32 < f.pairs ? (int)((min(p0 + wave * 32 + 32, f.pairs) - 1) / a.group) : INT_MIN / 2;      // ... and last one
+        const int wave_first = battn_same((int)((p0 + wave * 32) / a.group));                                     // the wavefront's first row
+        const int wave_last = battn_same(p0 + wave * 32 < f.pairs ? (int)((min(p0 + wave * 32 + 32, f.pairs) - 1) / a.group) : INT_MIN / 2);      // ... and last one
         const long long pair = min(p0 + wave * 32 + col, f.pairs - 1);
         const bool live = p0 + wave * 32 + col < f.pairs;
         const int row = (int)(pair / a.group), g = (int)(pair - (long long)row * a.group);
@@ -238,15 +239,19 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
         for (int t = 0; t < DT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-        for (int c = b0; c < b1; ++c, buf ^= 1) {
-            if (len <= 0) continue;                           // (nothing to see; the same for all)
+        // block c is here, nobody reads block c-1 any more, and the next one is on its way
+        auto arrive = [&](int c) __attribute__((always_inline)) {
             battn_wait<0>();
-            battn_meet();                                     // block c is here and nobody reads block c-1 any more
+            battn_meet();
             if (c + 1 < b1) {
                 issue(c + 1, buf ^ 1);
                 look_up(c + 2);
             }
-            if (c * BT_CH > base + wave_last) continue;       // beyond all of the wavefront's rows
+        };
+        const int stop = len > 0 ? b1 : b0;                   // (a request without positions: nothing to see)
+        const int mine = max(b0, min(stop, (base + wave_last) / BT_CH + (base + wave_last >= 0)));       // blocks from here on lie behind all of the wavefront's rows
+        for (int c = b0; c < mine; ++c, buf ^= 1) {
+            arrive(c);
             const unsigned int bl = buf * 2 * KV;
             f32x16_t s[2];
 #pragma unroll
@@ -317,6 +322,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
                 }
             }
         }
+        for (int c = mine; c < stop; ++c, buf ^= 1) arrive(c);
         l += lane_xor(l, 32);
         const bool whole = b0 == 0 && b1 == n_blocks;
         const int out_row = r0 + row, out_kvh = kvh;
@@ -329,7 +335,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
         const int slot = 2 * run + (b0 == 0);
         // on to the next tile: its first block is on its way while this one is written (the buffer that it goes to has been read by all)
         if constexpr (PAGED) {
-            before += f.step + min((long long)(tile + 1) * BT_PAIRS, f.pairs);
+            before = battn_same(before + f.step + min((long long)(tile + 1) * BT_PAIRS, f.pairs));
             goes_on = before < end;
             if (goes_on) {
                 at = before;

@@ -164,7 +164,7 @@ extern "C" int32_t knnssd_paged_attention(const knnssd_pages *p, const int32_t *
     BattnArgs a{};
     a.q = q_dev; a.k = p->k_dev; a.v = p->v_dev; a.out = out_dev; a.q_stride = q_stride; a.out_stride = out_stride;
     a.page_stride = p->page_stride; a.head_stride = p->head_stride; a.pos_stride = p->pos_stride;
-    a.table = block_table_dev; a.row_start = row_start_dev; a.kv_len = kv_len_dev;
+    a.table = (const_ints)(uintptr_t)block_table_dev; a.row_start = (const_ints)(uintptr_t)row_start_dev; a.kv_len = (const_ints)(uintptr_t)kv_len_dev;
     a.n_requests = n_requests; a.n_rows = n_rows; a.width = table_width; a.shift = log2_of(p->page_size); a.n_pages = p->n_pages;
     a.H = n_heads; a.Hkv = p->n_kv_heads; a.group = n_heads / p->n_kv_heads;
     a.scale2 = scale * 1.4426950408889634f;
@@ -186,7 +186,7 @@ extern "C" int32_t knnssd_prompt_attention(const void *q_dev, int64_t q_stride, 
     if (k_stride > MAX_ROW_STRIDE || v_stride > MAX_ROW_STRIDE) return KNNSSD_ESHAPE;
     BattnArgs a{};
     a.q = q_dev; a.k = k_dev; a.v = v_dev; a.out = out_dev; a.q_stride = q_stride; a.out_stride = out_stride; a.k_stride = k_stride; a.v_stride = v_stride;
-    a.row_start = row_start_dev; a.n_requests = n_requests; a.n_rows = n_rows;
+    a.row_start = (const_ints)(uintptr_t)row_start_dev; a.n_requests = n_requests; a.n_rows = n_rows;
     a.H = n_heads; a.Hkv = n_kv_heads; a.group = n_heads / n_kv_heads;
     a.scale2 = scale * 1.4426950408889634f;
     if (head_dim == 128) launch_battn<128, false>(a, dtype, dtype, 0, (hipStream_t)hip_stream);
