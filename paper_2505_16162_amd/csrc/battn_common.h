@@ -19,7 +19,6 @@ struct BattnArgs {
     int n_requests, n_rows, width, shift, n_pages;
     int H, Hkv, group;
     float scale2;                               // scale * log2(e): softmax in powers of two
-    int few_rows;                               // requests of up to so many rows are battn_few_kernel's
     void *ws;
 };
 

@@ -7,7 +7,7 @@
 namespace ks {
 
 // ------------------------------------------------------------------------------------------
-// Few rows over a bf16 cache: what bounds them is the cache, read once. A request's (row, head) pairs of one kv head, 16 NT at a time, against
+// Few rows over a bf16 cache: what bounds them is the cache, read once. A request's (row, head) pairs of one kv head, 16 at a time, against
 // all of its positions are a group; a group's blocks of 32 (heads of 64: 64) positions are units, and the units of the whole batch, group behind
 // group, are dealt to the workgroups in equal runs (worked out by each for itself from the lengths). The four wavefronts of a workgroup take the
 // blocks of a run in turn, keys and values straight from the cache to registers as operands, and are merged in LDS where a group ends. A
@@ -19,12 +19,12 @@ namespace ks {
 
 // positions of a unit: 8 KB of keys, 8 KB of values, which a wavefront holds in registers
 template <int HD> __host__ __device__ constexpr int battn_few_positions() { return 32 * 128 / HD; }
-// units of request r: rows (0: not this kernel's), blocks of a group, groups of pairs per kv head
+// units of request r: rows, blocks of a group, groups of pairs per kv head
 struct FewShape { int n, blocks, pair_groups; };
 __device__ __forceinline__ FewShape battn_few_shape(const BattnArgs &a, int r, int group_pairs, int positions) {
     FewShape f{0, 1, 0};
     const int n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
-    if (n > 0 && n <= a.few_rows) {
+    if (n > 0) {
         f.n = n;
         f.blocks = max(1, (battn_len(a, r) + positions - 1) / positions);
         f.pair_groups = (int)(((long long)n * a.group + group_pairs - 1) / group_pairs);
@@ -32,20 +32,11 @@ __device__ __forceinline__ FewShape battn_few_shape(const BattnArgs &a, int r, i
     return f;
 }
 
-template <int HD, int NT, int PW, int NP>
-__host__ __device__ constexpr int battn_few_lds() {
-    // the queries of a group [plane][pair][HD + 8] in bf16, and the wavefronts' shares [4][16][HD + BF_PAD] of one tile
-    return NP * PW * NT * 16 * (HD + 8) * 2 + 4 * 16 * (HD + BF_PAD) * 4;
-}
-
-// PW: most wavefronts that share a block, where the pairs are more than one holds
-template <int HD, int NT, int PW, int NP>
+template <int HD, int NP>
 __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
-    constexpr int QS = HD / 32, DT = HD / 16, QROW = HD + 8, MROW = HD + BF_PAD, PAIRS = 16 * NT * PW, CH = battn_few_positions<HD>(), PT = CH / 16;
+    constexpr int QS = HD / 32, DT = HD / 16, MROW = HD + BF_PAD, PAIRS = 16, CH = battn_few_positions<HD>(), PT = CH / 16;
     typedef unsigned int vword __attribute__((ext_vector_type(DT / 2)));
-    extern __shared__ __align__(16) char lds[];
-    bf16_t *ql = (bf16_t *)lds;
-    float *mb = (float *)(lds + NP * PAIRS * QROW * 2);
+    __shared__ __align__(16) float mb[4 * 16 * MROW];         // the wavefronts' shares of a group
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kg = lane >> 4, n16 = lane & 15;
     float *slots = (float *)((char *)a.ws + battn_few_merges());
@@ -98,15 +89,14 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
     // Where the run is: a group, its blocks [b0, b1) of the run. What follows sets these for the blocks from `unit` on, and requests the group's
     // queries and the wavefront's first block.
     FewShape f = battn_few_shape(a, r, PAIRS, CH);
-    int kvh, pg, b0, b1, r0, len, last, pairs, wp, wb, step, wave_pair;
+    int kvh, pg, b0, b1, r0, len, last, pairs;
     bool any;
     const_ints table;
     const bf16_t *kb, *vb;
     u32x4_t kf[PT][QS];                                       // position 16 pt + n16, dimensions 32 ks + 8 kg ...
     vword vr[PT][4];                                          // position 16 pt + 4 kg + i, dimensions DT n16 ...
     int page[PT][2];
-    constexpr int NQ = (PAIRS * (HD / 8) + 255) / 256;        // 8 values of a query each: a thread's
-    u32x4_t qv[NQ][NP == 1 ? 1 : 2];
+    u32x4_t qv[QS][NP == 1 ? 1 : 2];                          // the next group's queries: pair n16, dimensions 32 ks + 8 kg ...
     // first position of the block's e-th eight of tile pt (a page holds at least eight); positions past the last one repeat it
     auto eight = [&](int b, int pt, int e) __attribute__((always_inline)) { return min(b * CH + pt * 16 + e * 8, last & -8); };
     auto look_up = [&](int b) __attribute__((always_inline)) {
@@ -139,6 +129,19 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
             for (int i = 0; i < 4; ++i) vr[pt][i] = *reinterpret_cast<const vword *>(vp + min((kg & 1) * 4 + i, rest) * a.pos_stride);
         }
     };
+    auto load_queries = [&]() __attribute__((always_inline)) {
+        const int pair = pg * PAIRS + min(n16, pairs - 1);
+        const long long at = (long long)(r0 + pair / a.group) * a.q_stride + (kvh * a.group + pair % a.group) * HD + kg * 8;
+#pragma unroll
+        for (int ks = 0; ks < QS; ++ks) {
+            if constexpr (NP == 1) {
+                qv[ks][0] = *reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + at + ks * 32);
+            } else {
+                qv[ks][0] = *reinterpret_cast<const u32x4_t *>((const float *)a.q + at + ks * 32);
+                qv[ks][1] = *reinterpret_cast<const u32x4_t *>((const float *)a.q + at + ks * 32 + 4);
+            }
+        }
+    };
     auto enter = [&]() __attribute__((always_inline)) {
         while (unit - before >= (long long)f.blocks * f.pair_groups * a.Hkv && r + 1 < a.n_requests) {   // on to the next request with units
             before += (long long)f.blocks * f.pair_groups * a.Hkv;
@@ -154,122 +157,85 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
         len = battn_same(battn_len(a, r));
         last = len - 1;
         pairs = min(PAIRS, f.n * a.group - pg * PAIRS);       // (rows times heads: at most those of a call)
-        // wavefronts that share a block, 16 NT pairs each; a wavefront's pairs; its blocks: wb, wb + step, ...
-        const int pw = PW == 1 || pairs <= 16 * NT ? 1 : PW;
-        wp = wave & (pw - 1); wb = wave / pw; step = 4 / pw; wave_pair = wp * 16 * NT;
         table = a.table + (size_t)r * a.width;
         kb = (const bf16_t *)a.k + kvh * a.head_stride;
         vb = (const bf16_t *)a.v + kvh * a.head_stride;
-        any = len > 0 && wave_pair < pairs && b0 + wb < b1;
-        if (any) look_up(b0 + wb);
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            const int p = (i * 256 + tid) / (HD / 8), d = (tid % (HD / 8)) * 8, pair = pg * PAIRS + min(p, pairs - 1);
-            const long long at = (long long)(r0 + pair / a.group) * a.q_stride + (kvh * a.group + pair % a.group) * HD + d;
-            if constexpr (NP == 1) {
-                qv[i][0] = *reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + at);
-            } else {
-                qv[i][0] = *reinterpret_cast<const u32x4_t *>((const float *)a.q + at);
-                qv[i][1] = *reinterpret_cast<const u32x4_t *>((const float *)a.q + at + 4);
-            }
-        }
+        any = len > 0 && b0 + wave < b1;
+        if (any) look_up(b0 + wave);
+        if constexpr (NP == 1) load_queries();                // (there is no room for fp32 ones beside the last group's)
         if (any) {
-            load_keys(b0 + wb);
-            load_values(b0 + wb);
-            look_up(b0 + wb + step);
+            load_keys(b0 + wave);
+            load_values(b0 + wave);
+            look_up(b0 + wave + 4);
         }
     };
     enter();
     while (true) {
-        const int base = len - f.n, pw = 4 / step;
-        __syncthreads();                                      // nobody reads the last group's queries any more
+        const int base = len - f.n;
+        const int limit = base + (pg * PAIRS + min(n16, pairs - 1)) / a.group, first_limit = base + pg * PAIRS / a.group;      // last visible position of the lane's pair, of the first
+        bf16x8_t qf[QS][NP];
+        if constexpr (NP == 3) load_queries();
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            if (PAIRS * (HD / 8) < 256 && tid >= PAIRS * (HD / 8)) break;
-            bf16_t *to = ql + ((i * 256 + tid) / (HD / 8)) * QROW + (tid % (HD / 8)) * 8;
+        for (int ks = 0; ks < QS; ++ks) {
             if constexpr (NP == 1) {
-                *reinterpret_cast<u32x4_t *>(to) = qv[i][0] ^ (flip | flip >> 16);
+                qf[ks][0] = __builtin_bit_cast(bf16x8_t, qv[ks][0] ^ (flip | flip >> 16));
             } else {
                 float v[8];
-                bf16x8_t planes[3];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(qv[i][e >> 2][e & 3] ^ flip);
-                battn_planes<3>(v, planes);
-#pragma unroll
-                for (int x = 0; x < 3; ++x) *reinterpret_cast<bf16x8_t *>(to + x * PAIRS * QROW) = planes[x];
+                for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(qv[ks][e >> 2][e & 3] ^ flip);
+                battn_planes<3>(v, qf[ks]);
             }
         }
-        __syncthreads();
-
-        int limit[NT];                                        // a pair's last visible position
-        float off[NT], l[NT];
-        f32x4_t o[NT][DT];
+        float off = -INFINITY, l = 0.f;
+        f32x4_t o[DT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            limit[t] = base + (pg * PAIRS + min(wave_pair + t * 16 + n16, pairs - 1)) / a.group;
-            off[t] = -INFINITY;
-            l[t] = 0.f;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        }
-        const int first_limit = base + pg * PAIRS / a.group;
+        for (int d = 0; d < DT; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         // (two builds, with a next block and without: what is in flight where a value is waited for has to be known)
         auto work = [&](int b, auto more_) __attribute__((always_inline)) {
             constexpr bool more = decltype(more_)::value;
             const int pos0 = b * CH;
-            const bool diagonal = pos0 + CH - 1 > first_limit;
-            f32x4_t s[NT][PT];
-            unsigned int qb = (unsigned int)(uintptr_t)BATTN_LDS(lds) + ((wave_pair + n16) * QROW + kg * 8) * 2;
-            if (NT * NP > 1) asm volatile("" : "+v"(qb));     // (they are read again for every block: there is no room to keep them all)
+            f32x4_t s[PT];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
+            for (int pt = 0; pt < PT; ++pt) s[pt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            // the lowest plane first
 #pragma unroll
-                for (int pt = 0; pt < PT; ++pt) s[t][pt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-                // the lowest plane first
+            for (int q = NP - 1; q >= 0; --q)
 #pragma unroll
-                for (int q = NP - 1; q >= 0; --q)
+                for (int ks = 0; ks < QS; ++ks)
 #pragma unroll
-                    for (int ks = 0; ks < QS; ++ks) {
-                        const bf16x8_t qf = *(__attribute__((address_space(3))) const bf16x8_t *)(uintptr_t)(qb + ((q * PAIRS + t * 16) * QROW + ks * 32) * 2);
+                    for (int pt = 0; pt < PT; ++pt) s[pt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[pt][ks]), qf[ks][q], s[pt], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (more) load_keys(b + 4);
+            __builtin_amdgcn_sched_barrier(0);
+            if (pos0 + CH - 1 > first_limit) {
 #pragma unroll
-                        for (int pt = 0; pt < PT; ++pt) s[t][pt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[pt][ks]), qf, s[t][pt], 0, 0, 0);
-                    }
+                for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (pos0 + pt * 16 + 4 * kg + i > limit) s[pt][i] = -INFINITY;
             }
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (more) load_keys(b + step);
-            __builtin_amdgcn_sched_barrier(0);
+            float cm = s[0][0];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                if (diagonal) {
+            for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
-                    for (int pt = 0; pt < PT; ++pt)
+                for (int i = 0; i < 4; ++i) cm = fmaxf(cm, s[pt][i]);
+            cm = fmaxf(cm, lane_xor(cm, 16));
+            cm = fmaxf(cm, lane_xor(cm, 32));
+            const float off_new = fmaxf(off, battn_rounded_product(cm, c2)), ref = off_new == -INFINITY ? 0.f : off_new;
+            const float fac = __builtin_amdgcn_exp2f(off - ref);
+            off = off_new;
+            float ps = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (pos0 + pt * 16 + 4 * kg + i > limit[t]) s[t][pt][i] = -INFINITY;
+            for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[pt][i] = __builtin_amdgcn_exp2f(fmaf(s[pt][i], c2, -ref));
+                    ps += s[pt][i];
                 }
-                float cm = s[t][0][0];
+            l = l * fac + ps;
+            if (__any(fac != 1.0f)) {
 #pragma unroll
-                for (int pt = 0; pt < PT; ++pt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) cm = fmaxf(cm, s[t][pt][i]);
-                cm = fmaxf(cm, lane_xor(cm, 16));
-                cm = fmaxf(cm, lane_xor(cm, 32));
-                const float off_new = fmaxf(off[t], battn_rounded_product(cm, c2)), ref = off_new == -INFINITY ? 0.f : off_new;
-                const float fac = __builtin_amdgcn_exp2f(off[t] - ref);
-                off[t] = off_new;
-                float ps = 0.f;
-#pragma unroll
-                for (int pt = 0; pt < PT; ++pt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        s[t][pt][i] = __builtin_amdgcn_exp2f(fmaf(s[t][pt][i], c2, -ref));
-                        ps += s[t][pt][i];
-                    }
-                l[t] = l[t] * fac + ps;
-                if (__any(fac != 1.0f)) {
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[t][d] *= fac;
-                }
+                for (int d = 0; d < DT; ++d) o[d] *= fac;
             }
             u32x4_t vf[PT / 2][DT];                           // the values' operands: positions 2j, 2j+1 of the lane's eight
 #pragma unroll
@@ -285,28 +251,25 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d) asm volatile("" : "+v"(vf[hf][d]));       // all of it here: the next values go to the same registers
             if constexpr (more) {
-                load_values(b + step);
-                look_up(b + 2 * step);
+                load_values(b + 4);
+                look_up(b + 8);
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int hf = 0; hf < PT / 2; ++hf) {
+                const f32x4_t x = s[2 * hf], y = s[2 * hf + 1];
+                const float pv[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+                bf16x8_t pb[NP];
+                battn_planes<NP>(pv, pb);
 #pragma unroll
-                for (int hf = 0; hf < PT / 2; ++hf) {
-                    const f32x4_t x = s[t][2 * hf], y = s[t][2 * hf + 1];
-                    const float pv[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-                    bf16x8_t pb[NP];
-                    battn_planes<NP>(pv, pb);
+                for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int d = 0; d < DT; ++d)
-#pragma unroll
-                        for (int q = NP - 1; q >= 0; --q)
-                            o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vf[hf][d]), pb[q], o[t][d], 0, 0, 0);
-                }
+                    for (int q = NP - 1; q >= 0; --q) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vf[hf][d]), pb[q], o[d], 0, 0, 0);
+            }
         };
         if (any) {
-            int b = b0 + wb;
-            for (; b + step < b1; b += step) work(b, std::true_type{});
+            int b = b0 + wave;
+            for (; b + 4 < b1; b += 4) work(b, std::true_type{});
             work(b, std::false_type{});
         }
 
@@ -317,48 +280,45 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
         unit += b1 - b0;
         if (goes_on) enter();
 
-        // the wavefronts' shares of each tile: thread (pair, dimensions) adds them up and writes them out, or leaves them for the merge
-        float *slot = slots + (size_t)(2 * w + begins) * battn_few_slot<HD>(PAIRS);
+        // the wavefronts' shares: thread (pair, dimensions) adds them up and writes them out, or leaves them for the merge
+        l += lane_xor(l, 16);
+        l += lane_xor(l, 32);
+        float *mine = mb + (wave * 16 + n16) * MROW;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            l[t] += lane_xor(l[t], 16);
-            l[t] += lane_xor(l[t], 32);
-            float *mine = mb + (wave * 16 + n16) * MROW;
+        for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int d = 0; d < DT; d += 4) *reinterpret_cast<f32x4_t *>(mine + DT * (4 * kg + q) + d) = f32x4_t{o[d][q], o[d + 1][q], o[d + 2][q], o[d + 3][q]};
+        if (kg == 0) { mine[HD] = off; mine[HD + 1] = l; }
+        __syncthreads();
+        constexpr int V = HD / 16;                            // values per thread
+        const int p = tid >> 4, d0 = (tid & 15) * V;
+        const float *share = mb + p * MROW;
+        float top = -INFINITY, sum = 0.f, v[V];
 #pragma unroll
-                for (int d = 0; d < DT; d += 4)
-                    *reinterpret_cast<f32x4_t *>(mine + DT * (4 * kg + q) + d) = f32x4_t{o[t][d][q], o[t][d + 1][q], o[t][d + 2][q], o[t][d + 3][q]};
-            if (kg == 0) { mine[HD] = off[t]; mine[HD + 1] = l[t]; }
-            __syncthreads();
-            constexpr int V = HD * PW / 16, TP = HD / V;      // values per thread, threads per pair
-            const int q16 = tid / TP, p = (q16 >> 4) * 16 * NT + t * 16 + (q16 & 15), d0 = (tid % TP) * V;
-            const float *share = mb + (((q16 >> 4) & (pw - 1)) * 16 + (q16 & 15)) * MROW;         // of the first of the wavefronts that have this pair
-            float top = -INFINITY, sum = 0.f, v[V];
-            for (int x = 0; x < 4; x += pw) top = fmaxf(top, share[x * 16 * MROW + HD]);
+        for (int x = 0; x < 4; ++x) top = fmaxf(top, share[x * 16 * MROW + HD]);
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = 0.f;
-            for (int x = 0; x < 4; x += pw) {
-                const float *m = share + x * 16 * MROW;
-                const float k = m[HD] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[HD] - top);
-                sum = fmaf(m[HD + 1], k, sum);
+        for (int e = 0; e < V; ++e) v[e] = 0.f;
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[e] = fmaf(m[d0 + e], k, v[e]);
+        for (int x = 0; x < 4; ++x) {
+            const float *m = share + x * 16 * MROW;
+            const float k = m[HD] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[HD] - top);
+            sum = fmaf(m[HD + 1], k, sum);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = fmaf(m[d0 + e], k, v[e]);
+        }
+        if (p < this_pairs) {
+            if (whole) {
+                battn_few_out<V, HD, NP>(a, this_r0, this_kvh, this_pair + p, d0, v, sum);
+            } else {
+                float *to = slots + (size_t)(2 * w + begins) * battn_few_slot<HD>(PAIRS) + p * MROW;
+                store_values<V>(to + d0, v);
+                if (d0 == 0) { to[HD] = top; to[HD + 1] = sum; }
             }
-            if (p < this_pairs && q16 < 16 * pw) {
-                if (whole) {
-                    battn_few_out<V, HD, NP>(a, this_r0, this_kvh, this_pair + p, d0, v, sum);
-                } else {
-                    float *to = slot + p * MROW;
-                    store_values<V>(to + d0, v);
-                    if (d0 == 0) { to[HD] = top; to[HD + 1] = sum; }
-                }
-            }
-            __syncthreads();
         }
         if (!whole && begins && tid == 0)                     // it goes on in the runs behind this one
             merges[w] = FewMerge{battn_run_of(group_end, q, rem) - w + 1, this_r0, this_kvh, this_pair, this_pairs};
         if (!goes_on) return;
+        __syncthreads();                                      // (the shares have been read)
     }
 }
 

@@ -28,7 +28,7 @@ __device__ __forceinline__ bool battn_find_tile(const BattnArgs &a, int index, i
         int mine = 0;
         if (r < a.n_requests) {
             const long long n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
-            if (n > a.few_rows) mine = (int)((n * a.group + BT_PAIRS - 1) / BT_PAIRS);
+            if (n > 0) mine = (int)((n * a.group + BT_PAIRS - 1) / BT_PAIRS);
         }
         int upto = mine;
         for (int off = 1; off < 64; off <<= 1) {
@@ -55,7 +55,7 @@ template <int HD> constexpr int battn_tile_lds() { return 2 * 2 * BT_CH * HD * 2
 // what its blocks of 64 positions hold, so a run that begins x into a tile begins with block x / (64 group) of it, and a run of
 // 64 group or more is never empty. The costs before a tile have a closed form.
 struct TileShape {
-    int n, tiles;                       // rows (0: not this kernel's), tiles of a kv head
+    int n, tiles;                       // rows, tiles of a kv head
     long long step, pairs;              // cost of a tile without its own pairs; all pairs
     __device__ __forceinline__ long long before(int t) const { return t * step + (long long)(BT_PAIRS / 2) * t * (t + 1); }      // (t < tiles)
     __device__ __forceinline__ long long total() const { return tiles ? before(tiles - 1) + step + pairs : 0; }
@@ -64,7 +64,7 @@ constexpr int BT_FAR = 1 << 24;         // positions beyond count as so many
 __device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r) {
     TileShape f{0, 0, 0, 0};
     const int n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
-    if (n > 0 && n > a.few_rows) {
+    if (n > 0) {
         f.n = n;
         f.pairs = (long long)n * a.group;
         f.tiles = (int)((f.pairs + BT_PAIRS - 1) / BT_PAIRS);
@@ -73,7 +73,8 @@ __device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r)
     return f;
 }
 
-template <int HD, bool PAGED>
+// NP = 3: fp32 queries over a bf16 cache, which stay exact as three bf16 planes, as do the weights.
+template <int HD, bool PAGED, int NP>
 __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
     constexpr int KS = HD / 16, DT = HD / 32, SL = HD / 8, RB = HD * 2, MROW = HD + BF_PAD;
     constexpr int KV = BT_CH * RB;                            // bytes of a block's keys (or values)
@@ -83,7 +84,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
     const int col = lane & 31, half = lane >> 5;
     const unsigned int l0 = (unsigned int)(uintptr_t)BATTN_LDS(lds);
     const float c2 = fmaxf(fabsf(a.scale2), FLT_MIN);         // (a hidden score, -inf, has to stay that under a scale of 0)
-    const unsigned int flip = a.scale2 < 0.f ? 0x80008000u : 0u;
+    const unsigned int flip = a.scale2 < 0.f ? 0x80000000u : 0u;
 
     int r = 0, kvh, tile;
     TileShape f{0, 0, 0, 0};
@@ -227,11 +228,21 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
         const bool live = p0 + wave * 32 + col < f.pairs;
         const int row = (int)(pair / a.group), g = (int)(pair - (long long)row * a.group);
         const int limit = base + row;                         // the lane's last visible position
-        bf16x8_t qf[KS];                                          // dimensions 16 ks + 8 half ... of the lane's pair
+        bf16x8_t qf[KS][NP];                                  // dimensions 16 ks + 8 half ... of the lane's pair
         {
-            const bf16_t *qp = (const bf16_t *)a.q + (long long)(r0 + row) * a.q_stride + (kvh * a.group + g) * HD + half * 8;
+            const long long q_at = (long long)(r0 + row) * a.q_stride + (kvh * a.group + g) * HD + half * 8;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(qp + ks * 16) ^ flip);
+            for (int ks = 0; ks < KS; ++ks) {
+                if constexpr (NP == 1) {
+                    qf[ks][0] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + q_at + ks * 16) ^ (flip | flip >> 16));
+                } else {
+                    const u32x4_t lo = *reinterpret_cast<const u32x4_t *>((const float *)a.q + q_at + ks * 16) ^ flip, hi = *reinterpret_cast<const u32x4_t *>((const float *)a.q + q_at + ks * 16 + 4) ^ flip;
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { v[e] = __uint_as_float(lo[e]); v[4 + e] = __uint_as_float(hi[e]); }
+                    battn_planes<3>(v, qf[ks]);
+                }
+            }
         }
         float ref = -INFINITY, l = 0.f;
         f32x16_t o[DT];
@@ -265,7 +276,8 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(__attribute__((address_space(3))) const u32x4_t *)(uintptr_t)(from + t * 32 * RB));
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s[t], 0, 0, 0);
+#pragma unroll
+                    for (int q = NP - 1; q >= 0; --q) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][q], s[t], 0, 0, 0);
                 }
             }
             if (c * BT_CH + BT_CH - 1 > base + wave_first) {  // some of the block's positions lie behind some of the wavefront's rows
@@ -311,14 +323,16 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
 #pragma unroll
             for (int st = 0; st < 4; ++st) {                  // 16 positions
                 const int t = st >> 1, i0 = (st & 1) * 8;
-                const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16(s[t][i0], s[t][i0 + 1]), pack_bf16(s[t][i0 + 2], s[t][i0 + 3]),
-                                                                         pack_bf16(s[t][i0 + 4], s[t][i0 + 5]), pack_bf16(s[t][i0 + 6], s[t][i0 + 7])});
+                const float pv[8] = {s[t][i0], s[t][i0 + 1], s[t][i0 + 2], s[t][i0 + 3], s[t][i0 + 4], s[t][i0 + 5], s[t][i0 + 6], s[t][i0 + 7]};
+                bf16x8_t pb[NP];
+                battn_planes<NP>(pv, pb);
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
                     const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)(from[dt] + st * 16 * RB));
                     const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)(from[dt] + st * 16 * RB + 8 * RB));
                     const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb, o[dt], 0, 0, 0);
+#pragma unroll
+                    for (int q = NP - 1; q >= 0; --q) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[q], o[dt], 0, 0, 0);
                 }
             }
         }
@@ -355,13 +369,14 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
         if (!live) {
         } else if (!PAGED || whole) {
             const float inv = l > 0.f ? 1.f / l : 0.f;
-            bf16_t *op = (bf16_t *)a.out + (long long)out_row * a.out_stride + (out_kvh * a.group + g) * HD + 4 * half;
+            const long long out_at = (long long)out_row * a.out_stride + (out_kvh * a.group + g) * HD + 4 * half;
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     const float v[4] = {o[t][4 * b] * inv, o[t][4 * b + 1] * inv, o[t][4 * b + 2] * inv, o[t][4 * b + 3] * inv};
-                    store_values<4>(op + t * 32 + b * 8, v);
+                    if constexpr (NP == 1) store_values<4>((bf16_t *)a.out + out_at + t * 32 + b * 8, v);
+                    else store_values<4>((float *)a.out + out_at + t * 32 + b * 8, v);
                 }
         } else {
             float *to = (float *)((char *)a.ws + battn_few_merges()) + (size_t)slot * battn_few_slot<HD>(BT_PAIRS) + (wave * 32 + col) * MROW;

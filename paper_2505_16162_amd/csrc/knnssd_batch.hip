@@ -82,60 +82,52 @@ static int32_t rows_check(const int32_t *row_start_dev, int32_t n_requests, cons
     return KNNSSD_OK;
 }
 
-template <int HD>
-static void launch_merge(const BattnArgs &a, bool fp32, unsigned runs, int pairs, int64_t groups, int slot_pairs, hipStream_t s) {
+template <int HD, int NP>
+static void launch_merge(const BattnArgs &a, unsigned runs, int pairs, int64_t groups, int slot_pairs, hipStream_t s) {
     // few groups lie in many runs each, whose pairs then take four teams of lanes
     const int at_once = groups < BF_WGS / 4 ? battn_merge_teams<HD>() / 4 : battn_merge_teams<HD>();
-    const dim3 grid(runs, (pairs + at_once - 1) / at_once);
-    if (fp32) hipLaunchKernelGGL((battn_merge_kernel<HD, 3>), grid, dim3(BM_NT), 0, s, a, slot_pairs);
-    else hipLaunchKernelGGL((battn_merge_kernel<HD, 1>), grid, dim3(BM_NT), 0, s, a, slot_pairs);
+    hipLaunchKernelGGL((battn_merge_kernel<HD, NP>), dim3(runs, (pairs + at_once - 1) / at_once), dim3(BM_NT), 0, s, a, slot_pairs);
 }
 
 // tiles at most; what is too much ends at once
 static int64_t tiles_bound(const BattnArgs &a) { return (((int64_t)a.n_rows * a.group + BT_PAIRS - 1) / BT_PAIRS + a.n_requests) * a.Hkv; }
 
-template <int HD>
-static void launch_paged_tiles(const BattnArgs &a, hipStream_t s) {
-    hipLaunchKernelGGL((battn_tile_kernel<HD, true>), dim3(BF_WGS), dim3(256), battn_tile_lds<HD>(), s, a);
-    launch_merge<HD>(a, false, BF_WGS, BT_PAIRS, tiles_bound(a), BT_PAIRS, s);
+template <int HD, int NP>
+static void launch_paged_tiles(const BattnArgs &a, int64_t most, hipStream_t s) {
+    hipLaunchKernelGGL((battn_tile_kernel<HD, true, NP>), dim3(BF_WGS), dim3(256), battn_tile_lds<HD>(), s, a);
+    launch_merge<HD, NP>(a, BF_WGS, (int)(most < BT_PAIRS ? most : BT_PAIRS), tiles_bound(a), BT_PAIRS, s);
 }
 
-// most (row, head) pairs of one kv head for which a request goes through battn_few_kernel where battn_tile_kernel is there too
-static const int FEW_PAIRS = 64;
+// most (row, head) pairs of one kv head that a request may have for battn_few_kernel to take the batch
+static const int FEW_PAIRS = 16;
 
-template <int HD, int NT, int PW, int NP>
+template <int HD, int NP>
 static void launch_few(const BattnArgs &a, int64_t most, hipStream_t s) {
     const int ch = battn_few_positions<HD>();
-    const int64_t blocks = (((int64_t)a.width << a.shift) + ch - 1) / ch, groups = ((int64_t)a.n_rows * a.group + 16 * NT * PW - 1) / (16 * NT * PW) + a.n_requests;
+    const int64_t blocks = (((int64_t)a.width << a.shift) + ch - 1) / ch, groups = ((int64_t)a.n_rows * a.group + FEW_PAIRS - 1) / (FEW_PAIRS) + a.n_requests;
     const int64_t units = blocks < INT32_MAX ? blocks * groups * a.Hkv : INT64_MAX;      // at most
     const unsigned runs = (unsigned)(units / 4 + 1 < BF_WGS ? units / 4 + 1 : BF_WGS);
-    hipLaunchKernelGGL((battn_few_kernel<HD, NT, PW, NP>), dim3(runs), dim3(256), (battn_few_lds<HD, NT, PW, NP>()), s, a);
-    launch_merge<HD>(a, NP == 3, runs, (int)(most < 16 * NT * PW ? most : 16 * NT * PW), groups * a.Hkv, 16 * NT * PW, s);
+    hipLaunchKernelGGL((battn_few_kernel<HD, NP>), dim3(runs), dim3(256), 0, s, a);
+    launch_merge<HD, NP>(a, runs, (int)(most < FEW_PAIRS ? most : FEW_PAIRS), groups * a.Hkv, FEW_PAIRS, s);
 }
 
 // attention over a bf16 cache
 template <int HD>
-static void launch_paged_bf16(BattnArgs a, int32_t dtype, int32_t most_rows, hipStream_t s) {
+static void launch_paged_bf16(const BattnArgs &a, int32_t dtype, int32_t most_rows, hipStream_t s) {
     const int64_t most = (int64_t)(most_rows > 0 && most_rows < a.n_rows ? most_rows : a.n_rows) * a.group;
-    a.few_rows = INT_MAX;
-    if (dtype == KNNSSD_FP32) {
-        if (most <= 16) launch_few<HD, 1, 1, 3>(a, most, s);
-        else launch_few<HD, 2, 1, 3>(a, most, s);
-        return;
+    if (most <= FEW_PAIRS) {
+        if (dtype == KNNSSD_FP32) launch_few<HD, 3>(a, most, s);
+        else launch_few<HD, 1>(a, most, s);
+    } else {
+        if (dtype == KNNSSD_FP32) launch_paged_tiles<HD, 3>(a, most, s);
+        else launch_paged_tiles<HD, 1>(a, most, s);
     }
-    if (most > FEW_PAIRS) a.few_rows = FEW_PAIRS / a.group;
-    if (a.few_rows > 0) {
-        if (most <= 16) launch_few<HD, 1, 1, 1>(a, most, s);
-        else if (most <= 32) launch_few<HD, 2, 1, 1>(a, most, s);
-        else launch_few<HD, 2, 2, 1>(a, most, s);
-    }
-    if (most > FEW_PAIRS) launch_paged_tiles<HD>(a, s);
 }
 
 template <int HD, bool PAGED>
 static void launch_battn(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, int32_t most_rows, hipStream_t s) {
     if (!PAGED && dtype == KNNSSD_BF16) {
-        hipLaunchKernelGGL((battn_tile_kernel<HD, false>), dim3((unsigned)tiles_bound(a)), dim3(256), battn_tile_lds<HD>(), s, a);
+        hipLaunchKernelGGL((battn_tile_kernel<HD, false, 1>), dim3((unsigned)tiles_bound(a)), dim3(256), battn_tile_lds<HD>(), s, a);
         return;
     }
     if (PAGED && kv_dtype == KNNSSD_BF16) return launch_paged_bf16<HD>(a, dtype, most_rows, s);
