@@ -126,6 +126,10 @@ __device__ __forceinline__ int battn_run_of(long long unit, long long q, long lo
     return (int)(unit < longer ? battn_divide(unit, q + 1) : rem + battn_divide(unit - longer, q));
 }
 
+// A workgroup's run. Workgroups are dealt round the eight XCDs; runs next to each other, which share keys and values or a group whose partial results are
+// joined, go to one of them (the grids are multiples of eight).
+__device__ __forceinline__ int battn_run() { return (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3)); }
+
 // V values of one pair, divided by the sum of its weights
 template <int V, int HD, int NP>
 __device__ __forceinline__ void battn_few_out(const BattnArgs &a, int r0, int kvh, int pair, int d, float *v, float sum) {
@@ -138,7 +142,7 @@ __device__ __forceinline__ void battn_few_out(const BattnArgs &a, int r0, int kv
 }
 
 // Joins the partial results of a group. HD/4 lanes have a pair, four values each, and take its runs' results one after the other, four requested at a
-// time; where the group lies in more than four runs, four such teams share them. In a launch of its own: the last workgroup of a group doing it inside
+// time; where the group lies in more than eight runs, four such teams share them. In a launch of its own: the last workgroup of a group doing it inside
 // the first launch had to fetch up to 32 runs' results of all pairs by itself, one memory latency after the other (two requests at
 // 100 000 positions: 286 us in all, 168 us in two launches).
 constexpr int BM_NT = 256;
@@ -148,15 +152,16 @@ __global__ __launch_bounds__(BM_NT) void battn_merge_kernel(BattnArgs a, int slo
     constexpr int LP = HD / 4, TEAMS = battn_merge_teams<HD>(), MROW = HD + BF_PAD, U = 4;
     __shared__ f32x4_t part[TEAMS][LP];
     __shared__ float part_top[TEAMS], part_sum[TEAMS];
-    const FewMerge m = ((const FewMerge *)a.ws)[blockIdx.x];
+    const int run = battn_run();
+    const FewMerge m = ((const FewMerge *)a.ws)[run];
     if (m.runs == 0) return;                                  // the whole workgroup
     const int lane = threadIdx.x % LP, team = threadIdx.x / LP;
-    const int subs = m.runs > 4 ? 4 : 1, sub = team & (subs - 1), at_once = TEAMS / subs;
+    const int subs = m.runs > 8 ? 4 : 1, sub = team & (subs - 1), at_once = TEAMS / subs;
     const size_t slot = battn_few_slot<HD>(slot_pairs);
     for (int p0 = blockIdx.y * at_once; p0 < m.pairs; p0 += gridDim.y * at_once) {
         const int p = p0 + team / subs;
         // run x's partial result is its second one (a group that begins there) for the first run, its first one for the others
-        const float *first = (const float *)((const char *)a.ws + battn_few_merges()) + 2 * blockIdx.x * slot + min(p, m.pairs - 1) * MROW;
+        const float *first = (const float *)((const char *)a.ws + battn_few_merges()) + 2 * run * slot + min(p, m.pairs - 1) * MROW;
         float top = -INFINITY, sum = 0.f;
         f32x4_t v{0.f, 0.f, 0.f, 0.f};
         for (int x = sub; x < m.runs; x += subs * U) {

@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
     // All units, the first of this workgroup's run, and the request that has it: how many units lie before that one's. Up to 64 requests are looked at once.
     long long total = 0, before = 0, unit = 0, unit_end = 0, q = 0, rem = 0;
     int r = 0, runs = 0;
-    const int w = blockIdx.x;
+    const int w = battn_run();
     if (tid == 0) merges[w] = FewMerge{0, 0, 0, 0, 0};
     auto run_start = [&](int i) { return battn_same(i * q + min((long long)i, rem)); };      // rem runs of q + 1 units, the others of q
     for (int pass = 0; pass < 2; ++pass) {

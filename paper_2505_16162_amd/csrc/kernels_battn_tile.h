@@ -93,8 +93,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
     int run = 0;
     const long long block_cost = 64ll * a.group;
     if constexpr (PAGED) {
-        // runs next to each other on one XCD (workgroups are dealt round the eight), where they share keys and values
-        run = (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3));
+        run = battn_run();
         if (tid == 0) ((FewMerge *)a.ws)[run] = FewMerge{0, 0, 0, 0, 0};
         long long total = 0;
         for (int pass = 0; pass < 2; ++pass) {

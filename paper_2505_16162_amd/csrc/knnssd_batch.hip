@@ -106,7 +106,7 @@ static void launch_few(const BattnArgs &a, int64_t most, hipStream_t s) {
     const int ch = battn_few_positions<HD>();
     const int64_t blocks = (((int64_t)a.width << a.shift) + ch - 1) / ch, groups = ((int64_t)a.n_rows * a.group + FEW_PAIRS - 1) / (FEW_PAIRS) + a.n_requests;
     const int64_t units = blocks < INT32_MAX ? blocks * groups * a.Hkv : INT64_MAX;      // at most
-    const unsigned runs = (unsigned)(units / 4 + 1 < BF_WGS ? units / 4 + 1 : BF_WGS);
+    const unsigned runs = (unsigned)(units / 4 + 1 < BF_WGS ? (units / 4 + 8) & -8 : BF_WGS);
     hipLaunchKernelGGL((battn_few_kernel<HD, NP>), dim3(runs), dim3(256), 0, s, a);
     launch_merge<HD, NP>(a, runs, (int)(most < FEW_PAIRS ? most : FEW_PAIRS), groups * a.Hkv, FEW_PAIRS, s);
 }
