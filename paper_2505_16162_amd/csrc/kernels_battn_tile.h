@@ -13,9 +13,7 @@ namespace ks {
 // accumulators of S^T (position 8(i/4) + 4(lane/32) + i%4 of pair lane%32 in register i) are, rounded and packed as they lie, the operand of the
 // second product, whose other operand takes the values' positions in the same order by transposing reads of LDS. Nothing is
 // exchanged between lanes but one maximum per block.
-// Keys and values come in blocks of 64 positions straight to LDS, one block ahead; 16-byte pieces of a row are stored in an order
-// (exclusive or with the row's number) in which neither the keys' reads (32 rows, two pieces each) nor the values' (4 rows, 32
-// bytes each) meet in a bank.
+// Keys and values come in blocks of 64 positions straight to LDS, one block ahead.
 // ------------------------------------------------------------------------------------------
 constexpr int BT_PAIRS = 128, BT_CH = 64;
 
@@ -154,7 +152,11 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
     const_ints table;
     // first row of the wavefront's i-th load of block c (rows past the request's last repeat that one)
     auto load_row = [&](int c, int i) __attribute__((always_inline)) { return min(c * BT_CH + (i * 4 + wave) * ROWS, last & -ROWS); };
-    const int kpiece = (lane % SL) ^ ((wave * ROWS + lane / SL) & (SL - 1)), vpiece = (lane % SL) ^ (((lane / SL) & 3) << 1);
+    // order of a row's 16-byte pieces (exclusive or with these), so that LDS reads do not meet in one of its 64 banks: the keys' are 32 rows, two pieces of each,
+    // the values' four rows, four pieces of each, at a time
+    auto key_order = [](int row) { return HD == 128 ? row & 15 : (row >> 1) & 7; };
+    auto value_order = [](int row) { return HD == 128 ? (row & 3) << 2 : (row & 2) << 1; };
+    const int kpiece = (lane % SL) ^ key_order(wave * ROWS + lane / SL), vpiece = (lane % SL) ^ value_order(lane / SL);
     int page[NI];
     auto look_up = [&](int c) __attribute__((always_inline)) {                               // the pages of block c
         if constexpr (PAGED)
@@ -182,11 +184,11 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
     // dimensions from 32 dt + 16 (lane / 16 % 2) + 4 (lane % 4)
     unsigned int k_at[KS], v_at[DT];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) k_at[ks] = l0 + col * RB + (((2 * ks + half) ^ (col & (SL - 1))) * 16);
+    for (int ks = 0; ks < KS; ++ks) k_at[ks] = l0 + col * RB + (((2 * ks + half) ^ key_order(col)) * 16);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
         const int v_row = 4 * half + ((lane & 15) >> 2), v_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-        v_at[dt] = l0 + KV + v_row * RB + (((4 * dt + (v_col >> 3)) ^ ((v_row & 3) << 1)) * 16) + (v_col & 4) * 2;
+        v_at[dt] = l0 + KV + v_row * RB + (((4 * dt + (v_col >> 3)) ^ value_order(v_row)) * 16) + (v_col & 4) * 2;
     }
     auto enter = [&]() __attribute__((always_inline)) {       // the segment of `tile` that begins at `at`
         r0 = max(a.row_start[r], 0);
