@@ -260,22 +260,15 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
                 look_up(c + 2);
             }
         };
-        const int stop = len > 0 ? b1 : b0;                   // (a request without positions: nothing to see)
-        const int mine = max(b0, min(stop, (base + wave_last) / BT_CH + (base + wave_last >= 0)));       // blocks from here on lie behind all of the wavefront's rows
-        for (int c = b0; c < mine; ++c, buf ^= 1) {
-            arrive(c);
-            const unsigned int bl = buf * 2 * KV;
-            f32x16_t s[2];
+        auto scores = [&](int c, f32x16_t *s) __attribute__((always_inline)) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                unsigned int from = k_at[ks] + bl;
-                asm("" : "+v"(from));                         // (one address, the tiles by the read's own offset)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
+                for (int ks = 0; ks < KS; ++ks) {
+                    unsigned int from = k_at[ks] + buf * 2 * KV;
+                    asm("" : "+v"(from));                     // (one address, the tiles by the read's own offset)
                     const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(__attribute__((address_space(3))) const u32x4_t *)(uintptr_t)(from + t * 32 * RB));
 #pragma unroll
                     for (int q = NP - 1; q >= 0; --q) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][q], s[t], 0, 0, 0);
@@ -288,23 +281,22 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
                     for (int i = 0; i < 16; ++i)
                         if (c * BT_CH + t * 32 + 8 * (i / 4) + 4 * half + i % 4 > limit) s[t][i] = -INFINITY;
             }
+        };
+        // the reference becomes the largest score
+        auto follow = [&](const f32x16_t *s) __attribute__((always_inline)) {
             float cm = s[0][0];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) cm = fmaxf(cm, s[t][i]);
             cm = fmaxf(cm, lane_xor(cm, 32));
-            // The reference that the weights are taken against follows the largest score only where that has left it 2^8 behind, and then for all lanes:
-            // weights of up to 2^8 lose nothing (bf16 and fp32 have the same steps there), and what has been summed up is rescaled a few
-            // times in all, instead of in every block in which one of 32 pairs has a new largest score.
-            const float top = battn_rounded_product(cm, c2);
-            if (__builtin_expect(__any(top > ref + 8.f), 0)) {
-                const float now = fmaxf(ref, top), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
-                ref = now;
-                l *= f;
+            const float now = fmaxf(ref, battn_rounded_product(cm, c2)), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
+            ref = now;
+            l *= f;
 #pragma unroll
-                for (int t = 0; t < DT; ++t) o[t] *= f;
-            }
+            for (int t = 0; t < DT; ++t) o[t] *= f;
+        };
+        auto weigh = [&](f32x16_t *s) __attribute__((always_inline)) {
             const float off = ref == -INFINITY ? 0.f : ref;
             float ps = 0.f;
 #pragma unroll
@@ -314,11 +306,27 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
                     s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], c2, -off));
                     ps += s[t][i];
                 }
+            return ps;
+        };
+        // The weights are taken against the largest score of the tile's first block: what comes later may be far above that (weights of up to
+        // 2^64 lose nothing, bf16 and fp32 have the same steps there) before the reference has to follow. So a block's
+        // weights wait for no maximum; a block whose sum shows that it should have been looked for is begun anew.
+        auto work = [&](int c, auto first_) __attribute__((always_inline)) {
+            constexpr bool FIRST = decltype(first_)::value;
+            f32x16_t s[2];
+            scores(c, s);
+            if constexpr (FIRST) follow(s);
+            float ps = weigh(s);
+            if (!FIRST && __builtin_expect(__any(ps > 0x1p64f), 0)) {
+                scores(c, s);
+                follow(s);
+                ps = weigh(s);
+            }
             l += ps;
             unsigned int from[DT];
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
-                from[dt] = v_at[dt] + bl;
+                from[dt] = v_at[dt] + buf * 2 * KV;
                 asm("" : "+v"(from[dt]));
             }
 #pragma unroll
@@ -335,6 +343,17 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
 #pragma unroll
                     for (int q = NP - 1; q >= 0; --q) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[q], o[dt], 0, 0, 0);
                 }
+            }
+        };
+        const int stop = len > 0 ? b1 : b0;                   // (a request without positions: nothing to see)
+        const int mine = max(b0, min(stop, (base + wave_last) / BT_CH + (base + wave_last >= 0)));       // blocks from here on lie behind all of the wavefront's rows
+        if (b0 < mine) {
+            arrive(b0);
+            work(b0, std::true_type{});
+            buf ^= 1;
+            for (int c = b0 + 1; c < mine; ++c, buf ^= 1) {
+                arrive(c);
+                work(c, std::false_type{});
             }
         }
         for (int c = mine; c < stop; ++c, buf ^= 1) arrive(c);
