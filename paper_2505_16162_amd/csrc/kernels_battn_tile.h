@@ -15,7 +15,10 @@ namespace ks {
 // exchanged between lanes but one maximum per block.
 // Keys and values come in blocks of 64 positions straight to LDS, one block ahead.
 // ------------------------------------------------------------------------------------------
-constexpr int BT_PAIRS = 128, BT_CH = 64;
+constexpr int BT_PAIRS = 128;
+// positions of a block: 64, or 32 over prompts in heads of 128, where the registers of a block's scores then leave room for a third wavefront on each SIMD
+// (two prompts of 4096 rows 418 -> 400 us; over pages, whose wavefronts need more of them, 512 -> 522 us)
+template <int HD, bool PAGED> constexpr int battn_tile_positions() { return HD == 128 && !PAGED ? 32 : 64; }
 
 // Tile `index` of the batch: its request and its number in there; false behind the last. Every wavefront for itself, 64 requests at a time.
 __device__ __forceinline__ bool battn_find_tile(const BattnArgs &a, int index, int &r_out, int &tile_out, int &tiles_out) {
@@ -46,7 +49,7 @@ __device__ __forceinline__ bool battn_find_tile(const BattnArgs &a, int index, i
     return false;
 }
 
-template <int HD> constexpr int battn_tile_lds() { return 2 * 2 * BT_CH * HD * 2; }
+template <int HD, bool PAGED> constexpr int battn_tile_lds() { return 2 * 2 * battn_tile_positions<HD, PAGED>() * HD * 2; }
 
 // Over pages the batch's tiles are dealt to the workgroups in equal runs, as in battn_few_kernel, by their cost: a tile's is the positions before its request's
 // new rows and those of its own pairs, times the heads of a group (in a pair's rows counted exactly: base * group + the pairs up to its last). It is at most
@@ -73,9 +76,9 @@ __device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r)
 
 // NP = 3: fp32 queries over a bf16 cache, which stay exact as three bf16 planes, as do the weights.
 template <int HD, bool PAGED, int NP>
-__global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
+__global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_kernel(BattnArgs a) {
     constexpr int KS = HD / 16, DT = HD / 32, SL = HD / 8, RB = HD * 2, MROW = HD + BF_PAD;
-    constexpr int KV = BT_CH * RB;                            // bytes of a block's keys (or values)
+    constexpr int CH = battn_tile_positions<HD, PAGED>(), KV = CH * RB;                             // bytes of a block's keys (or values)
     constexpr int ROWS = 64 / SL, NI = KV / 1024 / 4;         // rows a wavefront's load covers, loads per wavefront for the keys
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -89,7 +92,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
     // the run: where it is and where it ends, in cost; the cost before the tile
     long long at = 0, end = 0, before = 0, run_q = 0, run_rem = 0;
     int run = 0;
-    const long long block_cost = 64ll * a.group;
+    const long long block_cost = (long long)CH * a.group;
     if constexpr (PAGED) {
         run = battn_run();
         if (tid == 0) ((FewMerge *)a.ws)[run] = FewMerge{0, 0, 0, 0, 0};
@@ -151,7 +154,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
     const bf16_t *kb, *vb;
     const_ints table;
     // first row of the wavefront's i-th load of block c (rows past the request's last repeat that one)
-    auto load_row = [&](int c, int i) __attribute__((always_inline)) { return min(c * BT_CH + (i * 4 + wave) * ROWS, last & -ROWS); };
+    auto load_row = [&](int c, int i) __attribute__((always_inline)) { return min(c * CH + (i * 4 + wave) * ROWS, last & -ROWS); };
     // order of a row's 16-byte pieces (exclusive or with these), so that LDS reads do not meet in one of its 64 banks: the keys' are 32 rows, two pieces of each,
     // the values' four rows, four pieces of each, at a time
     auto key_order = [](int row) { return HD == 128 ? row & 15 : (row >> 1) & 7; };
@@ -197,7 +200,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
         last = len - 1;
         base = len - n;                                       // position of the request's first new row
         const int tile_last = battn_same((int)((min((long long)(tile + 1) * BT_PAIRS, f.pairs) - 1) / a.group));
-        n_blocks = (max(base, 0) + tile_last) / BT_CH + 1;
+        n_blocks = (max(base, 0) + tile_last) / CH + 1;
         b0 = 0;
         b1 = n_blocks;
         kb = (const bf16_t *)a.k;
@@ -262,7 +265,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
         };
         auto scores = [&](int c, f32x16_t *s) __attribute__((always_inline)) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < CH / 32; ++t) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
 #pragma unroll
@@ -274,19 +277,19 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
                     for (int q = NP - 1; q >= 0; --q) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][q], s[t], 0, 0, 0);
                 }
             }
-            if (c * BT_CH + BT_CH - 1 > base + wave_first) {  // some of the block's positions lie behind some of the wavefront's rows
+            if (c * CH + CH - 1 > base + wave_first) {  // some of the block's positions lie behind some of the wavefront's rows
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < CH / 32; ++t)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (c * BT_CH + t * 32 + 8 * (i / 4) + 4 * half + i % 4 > limit) s[t][i] = -INFINITY;
+                        if (c * CH + t * 32 + 8 * (i / 4) + 4 * half + i % 4 > limit) s[t][i] = -INFINITY;
             }
         };
         // the reference becomes the largest score
         auto follow = [&](const f32x16_t *s) __attribute__((always_inline)) {
             float cm = s[0][0];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < CH / 32; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) cm = fmaxf(cm, s[t][i]);
             cm = fmaxf(cm, lane_xor(cm, 32));
@@ -300,7 +303,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
             const float off = ref == -INFINITY ? 0.f : ref;
             float ps = 0.f;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < CH / 32; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], c2, -off));
@@ -313,7 +316,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
         // weights wait for no maximum; a block whose sum shows that it should have been looked for is begun anew.
         auto work = [&](int c, auto first_) __attribute__((always_inline)) {
             constexpr bool FIRST = decltype(first_)::value;
-            f32x16_t s[2];
+            f32x16_t s[CH / 32];
             scores(c, s);
             if constexpr (FIRST) follow(s);
             float ps = weigh(s);
@@ -330,7 +333,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
                 asm("" : "+v"(from[dt]));
             }
 #pragma unroll
-            for (int st = 0; st < 4; ++st) {                  // 16 positions
+            for (int st = 0; st < CH / 16; ++st) {                  // 16 positions
                 const int t = st >> 1, i0 = (st & 1) * 8;
                 const float pv[8] = {s[t][i0], s[t][i0 + 1], s[t][i0 + 2], s[t][i0 + 3], s[t][i0 + 4], s[t][i0 + 5], s[t][i0 + 6], s[t][i0 + 7]};
                 bf16x8_t pb[NP];
@@ -346,7 +349,7 @@ __global__ __launch_bounds__(256, 2) void battn_tile_kernel(BattnArgs a) {
             }
         };
         const int stop = len > 0 ? b1 : b0;                   // (a request without positions: nothing to see)
-        const int mine = max(b0, min(stop, (base + wave_last) / BT_CH + (base + wave_last >= 0)));       // blocks from here on lie behind all of the wavefront's rows
+        const int mine = max(b0, min(stop, (base + wave_last) / CH + (base + wave_last >= 0)));       // blocks from here on lie behind all of the wavefront's rows
         if (b0 < mine) {
             arrive(b0);
             work(b0, std::true_type{});

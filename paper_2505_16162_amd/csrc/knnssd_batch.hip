@@ -94,7 +94,7 @@ static int64_t tiles_bound(const BattnArgs &a) { return (((int64_t)a.n_rows * a.
 
 template <int HD, int NP>
 static void launch_paged_tiles(const BattnArgs &a, int64_t most, hipStream_t s) {
-    hipLaunchKernelGGL((battn_tile_kernel<HD, true, NP>), dim3(BF_WGS), dim3(256), battn_tile_lds<HD>(), s, a);
+    hipLaunchKernelGGL((battn_tile_kernel<HD, true, NP>), dim3(BF_WGS), dim3(256), (battn_tile_lds<HD, true>()), s, a);
     launch_merge<HD, NP>(a, BF_WGS, (int)(most < BT_PAIRS ? most : BT_PAIRS), tiles_bound(a), BT_PAIRS, s);
 }
 
@@ -127,7 +127,7 @@ static void launch_paged_bf16(const BattnArgs &a, int32_t dtype, int32_t most_ro
 template <int HD, bool PAGED>
 static void launch_battn(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, int32_t most_rows, hipStream_t s) {
     if (!PAGED && dtype == KNNSSD_BF16) {
-        hipLaunchKernelGGL((battn_tile_kernel<HD, false, 1>), dim3((unsigned)tiles_bound(a)), dim3(256), battn_tile_lds<HD>(), s, a);
+        hipLaunchKernelGGL((battn_tile_kernel<HD, false, 1>), dim3((unsigned)tiles_bound(a)), dim3(256), (battn_tile_lds<HD, false>()), s, a);
         return;
     }
     if (PAGED && kv_dtype == KNNSSD_BF16) return launch_paged_bf16<HD>(a, dtype, most_rows, s);
