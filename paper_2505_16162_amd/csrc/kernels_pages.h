@@ -6,8 +6,8 @@
 namespace ks {
 
 constexpr int PLAN_MAX_REQUESTS = 4096;                       // what the plan keeps in LDS
-constexpr int PLAN_NT = 1024, PLAN_PER = PLAN_MAX_REQUESTS / PLAN_NT;
 constexpr int PLAN_ROWS_NT = 256;
+constexpr int PLAN_U = 4;                                     // pages a thread has under way
 
 struct PlanArgs {
     int *table, *held, *free_pages, *n_free;
@@ -43,8 +43,10 @@ __device__ __forceinline__ void plan_row(const PlanArgs &a, const int *row_at, i
 // One workgroup. Per request the pages it needs, gives back and takes; three prefix sums (rows, pages back, pages taken) turn
 // the stack into arithmetic: the k-th page given back (ascending) is pushed to n_free + n_back - 1 - k, the k-th page taken is popped
 // from n_free + n_back - 1 - k, whatever it was. Nothing is changed before the totals have shown that all of it can be done.
+template <int PLAN_NT, int PLAN_PER>
 __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(PlanArgs a) {
-    __shared__ int row_at[PLAN_MAX_REQUESTS + 1], back_at[PLAN_MAX_REQUESTS + 1], take_at[PLAN_MAX_REQUESTS + 1];
+    constexpr int MOST = PLAN_NT * PLAN_PER;
+    __shared__ int row_at[MOST + 1], back_at[MOST + 1], take_at[MOST + 1];
     __shared__ long long wave_sums[PLAN_NT / 64][3];
     __shared__ int wave_max[PLAN_NT / 64], wave_bad[PLAN_NT / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -85,16 +87,27 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(PlanArgs a) {
     }
     if (lane == 0) { wave_max[wave] = longest; wave_bad[wave] = bad; }
     __syncthreads();
-    long long total[3] = {0, 0, 0};
-    for (int w = 0; w < PLAN_NT / 64; ++w) {
+    // the same over the wavefronts, a lane each
+    constexpr int NW = PLAN_NT / 64;
+    long long total[3];
 #pragma unroll
-        for (int q = 0; q < 3; ++q) {
-            const long long v = wave_sums[w][q];
-            if (w < wave) before[q] += v;
-            total[q] += v;
+    for (int q = 0; q < 3; ++q) {
+        const long long own = wave_sums[lane % NW][q];
+        long long v = own;
+#pragma unroll
+        for (int off = 1; off < NW; off <<= 1) {
+            const long long u = __shfl_up(v, off, NW);
+            if (lane % NW >= off) v += u;
         }
-        bad |= wave_bad[w];
-        longest = max(longest, wave_max[w]);
+        before[q] += __shfl(v - own, wave);
+        total[q] = __shfl(v, NW - 1);
+    }
+    bad |= wave_bad[lane % NW];
+    longest = max(longest, wave_max[lane % NW]);
+#pragma unroll
+    for (int off = 1; off < NW; off <<= 1) {
+        bad |= __shfl_xor(bad, off);
+        longest = max(longest, __shfl_xor(longest, off));
     }
     if (n_free + total[1] > a.n_pages) bad |= 1;
     if (total[0] > a.max_rows) bad |= 2;
@@ -121,24 +134,42 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(PlanArgs a) {
         }
         before[0] += rows[i]; before[1] += back[i]; before[2] += take[i];
     }
-    if (tid == PLAN_NT - 1 && a.n == PLAN_MAX_REQUESTS) {
+    if (tid == PLAN_NT - 1 && a.n == MOST) {
         row_at[a.n] = (int)total[0]; back_at[a.n] = n_back; take_at[a.n] = n_take;
         a.row_start[a.n] = (int)total[0];
     }
     __syncthreads();
-    for (int k = tid; k < n_back; k += PLAN_NT) {
-        const int r = plan_owner(back_at, a.n, k);
-        const int need = (int)(((long long)a.cached[r] + a.added[r] + page - 1) >> a.shift);
-        int *entry = a.table + (size_t)r * a.width + need + (k - back_at[r]);
-        a.free_pages[top - 1 - k] = *entry;
-        *entry = -1;
+    for (int k0 = tid; k0 < n_back; k0 += PLAN_U * PLAN_NT) {
+        int *entry[PLAN_U], page_id[PLAN_U];
+#pragma unroll
+        for (int u = 0; u < PLAN_U; ++u) {
+            const int k = min(k0 + u * PLAN_NT, n_back - 1), r = plan_owner(back_at, a.n, k);
+            const int need = (int)(((long long)a.cached[r] + a.added[r] + page - 1) >> a.shift);
+            entry[u] = a.table + (size_t)r * a.width + need + (k - back_at[r]);
+            page_id[u] = *entry[u];
+        }
+#pragma unroll
+        for (int u = 0; u < PLAN_U; ++u)
+            if (k0 + u * PLAN_NT < n_back) {
+                a.free_pages[top - 1 - (k0 + u * PLAN_NT)] = page_id[u];
+                *entry[u] = -1;
+            }
     }
     __syncthreads();
-    for (int k = tid; k < n_take; k += PLAN_NT) {
-        const int r = plan_owner(take_at, a.n, k);
-        int *from = a.free_pages + top - 1 - k;
-        a.table[(size_t)r * a.width + a.held[r] + (k - take_at[r])] = *from;
-        *from = -1;
+    for (int k0 = tid; k0 < n_take; k0 += PLAN_U * PLAN_NT) {
+        int *entry[PLAN_U], page_id[PLAN_U];
+#pragma unroll
+        for (int u = 0; u < PLAN_U; ++u) {
+            const int k = min(k0 + u * PLAN_NT, n_take - 1), r = plan_owner(take_at, a.n, k);
+            entry[u] = a.table + (size_t)r * a.width + a.held[r] + (k - take_at[r]);
+            page_id[u] = a.free_pages[top - 1 - k];
+        }
+#pragma unroll
+        for (int u = 0; u < PLAN_U; ++u)
+            if (k0 + u * PLAN_NT < n_take) {
+                *entry[u] = page_id[u];
+                a.free_pages[top - 1 - (k0 + u * PLAN_NT)] = -1;
+            }
     }
     __syncthreads();
 #pragma unroll

@@ -28,9 +28,13 @@ extern "C" int32_t knnssd_page_plan(const knnssd_page_tables *t, const int32_t *
     a.cached = cached_dev; a.added = added_dev;
     a.row_start = rows->row_start_dev; a.kv_len = rows->kv_len_dev; a.slots = rows->slots_dev; a.positions = rows->positions_dev; a.result = rows->result_dev;
     a.n = t->n_requests; a.width = t->table_width; a.n_pages = t->n_pages; a.shift = log2_of(t->page_size); a.max_rows = rows->max_rows;
-    a.rows_here = rows->max_rows <= 2 * PLAN_NT;
+    a.rows_here = rows->max_rows <= 2048;
     hipStream_t s = (hipStream_t)hip_stream;
-    hipLaunchKernelGGL(page_plan_kernel, dim3(1), dim3(PLAN_NT), 0, s, a);
+    // Few wavefronts meet sooner (48 requests: 5.4 us, with 1024 threads 8.6), many move pages faster (256 prompts admitted, 12 000 pages: 15 us, with 256 threads 36).
+    // No more pages change hands than the table has entries.
+    if (a.n <= 256 && a.rows_here && (int64_t)a.n * a.width <= 8192) hipLaunchKernelGGL((page_plan_kernel<256, 1>), dim3(1), dim3(256), 0, s, a);
+    else if (a.n <= 1024) hipLaunchKernelGGL((page_plan_kernel<1024, 1>), dim3(1), dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((page_plan_kernel<1024, 4>), dim3(1), dim3(1024), 0, s, a);
     if (!a.rows_here) {
         const int wgs = (int)(((int64_t)rows->max_rows + PLAN_ROWS_NT - 1) / PLAN_ROWS_NT);
         hipLaunchKernelGGL(page_rows_kernel, dim3(wgs < 1024 ? wgs : 1024), dim3(PLAN_ROWS_NT), 0, s, a);
