@@ -226,18 +226,19 @@ def _heads(t: torch.Tensor, device: torch.device, head_dim: int, name: str):
 def _call(device: torch.device, stream: Optional[torch.cuda.Stream], tensors, fn, *args) -> None:
     """fn(*args, stream) on the device's current stream or on `stream`, with that device current. The tensors stay with the
     allocator until what `stream` does with them is done."""
-    current = torch.cuda.current_stream(device)
-    if stream is None:
-        stream = current
-    elif stream != current:
+    handle = torch._C._cuda_getCurrentRawStream(device.index)     # (torch.cuda.current_stream takes 1.9 us of a call's 10)
+    if stream is not None and stream.cuda_stream != handle:
+        handle = stream.cuda_stream
         for t in tensors:
             if t is not None:
                 t.record_stream(stream)
     if torch.cuda.current_device() == device.index:
-        _check(fn(*args, stream.cuda_stream))
+        rc = fn(*args, handle)
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, stream.cuda_stream))
+            rc = fn(*args, handle)
+    if rc != 0:
+        _check(rc)
 
 
 class Pages:

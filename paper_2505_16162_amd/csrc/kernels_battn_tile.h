@@ -52,24 +52,27 @@ __device__ __forceinline__ bool battn_find_tile(const BattnArgs &a, int index, i
 template <int HD, bool PAGED> constexpr int battn_tile_lds() { return 2 * 2 * battn_tile_positions<HD, PAGED>() * HD * 2; }
 
 // Over pages the batch's tiles are dealt to the workgroups in equal runs, as in battn_few_kernel, by their cost: a tile's is the positions before its request's
-// new rows and those of its own pairs, times the heads of a group (in a pair's rows counted exactly: base * group + the pairs up to its last). It is at most
-// what its blocks of 64 positions hold, so a run that begins x into a tile begins with block x / (64 group) of it, and a run of
-// 64 group or more is never empty. The costs before a tile have a closed form.
+// new rows times the heads of a group, and the pairs up to its own last one (a pair's rows counted exactly), or a block's cost, positions of a block times heads
+// of a group, if that is more. It is at most what its blocks hold, so a run that begins x into a tile begins with block
+// x / (a block's cost) of it, and a run of a block's cost or more is never empty. The costs before a tile have a closed form.
 struct TileShape {
-    int n, tiles;                       // rows, tiles of a kv head
-    long long step, pairs;              // cost of a tile without its own pairs; all pairs
-    __device__ __forceinline__ long long before(int t) const { return t * step + (long long)(BT_PAIRS / 2) * t * (t + 1); }      // (t < tiles)
-    __device__ __forceinline__ long long total() const { return tiles ? before(tiles - 1) + step + pairs : 0; }
+    int n, tiles, small;                // rows, tiles of a kv head, those of its first that cost a block
+    long long step, pairs, block;       // cost of a tile without its own pairs; all pairs; a block's cost
+    __device__ __forceinline__ long long sloped(int t) const { return t * step + (long long)(BT_PAIRS / 2) * t * (t + 1); }
+    __device__ __forceinline__ long long before(int t) const { return t <= small ? t * block : small * block + sloped(t) - sloped(small); }      // (t < tiles)
+    __device__ __forceinline__ long long cost(int t) const { return max(block, step + min((long long)(t + 1) * BT_PAIRS, pairs)); }
+    __device__ __forceinline__ long long total() const { return tiles ? before(tiles - 1) + cost(tiles - 1) : 0; }
 };
 constexpr int BT_FAR = 1 << 24;         // positions beyond count as so many
-__device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r) {
-    TileShape f{0, 0, 0, 0};
+__device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r, int positions) {
+    TileShape f{0, 0, 0, 0, 0, (long long)positions * a.group};
     const int n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
     if (n > 0) {
         f.n = n;
         f.pairs = (long long)n * a.group;
         f.tiles = (int)((f.pairs + BT_PAIRS - 1) / BT_PAIRS);
         f.step = (long long)min(max(battn_len(a, r) - n, 0), BT_FAR) * a.group;
+        f.small = (int)min((long long)f.tiles, max(f.block - f.step, 0ll) / BT_PAIRS);
     }
     return f;
 }
@@ -88,7 +91,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
     const unsigned int flip = a.scale2 < 0.f ? 0x80000000u : 0u;
 
     int r = 0, kvh, tile;
-    TileShape f{0, 0, 0, 0};
+    TileShape f{0, 0, 0, 0, 0, 0};
     // the run: where it is and where it ends, in cost; the cost before the tile
     long long at = 0, end = 0, before = 0, run_q = 0, run_rem = 0;
     int run = 0;
@@ -101,7 +104,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
             bool found = false;
             for (int q0 = 0; q0 < a.n_requests && !found; q0 += 64) {
                 long long upto = 0;
-                if (q0 + lane < a.n_requests) upto = battn_tile_shape(a, q0 + lane).total() * a.Hkv;
+                if (q0 + lane < a.n_requests) upto = battn_tile_shape(a, q0 + lane, CH).total() * a.Hkv;
                 for (int off = 1; off < 64; off <<= 1) {
                     const long long u = __shfl_up(upto, off);
                     if (lane >= off) upto += u;
@@ -109,7 +112,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
                 if (pass == 0) total += battn_lane(upto, 63);
                 if (pass == 0 && q0 + 64 >= a.n_requests) {   // the total is known
                     if (total == 0) return;
-                    const int runs = battn_same((int)max(1ll, min((long long)gridDim.x, battn_divide(total, 2 * block_cost))));      // two blocks at least
+                    const int runs = battn_same((int)max(1ll, min((long long)gridDim.x, battn_divide(total, block_cost))));
                     if (run >= runs) return;
                     run_q = battn_divide(total, runs);
                     run_rem = total - run_q * runs;
@@ -130,7 +133,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
             }
             if (found) break;
         }
-        f = battn_tile_shape(a, r);
+        f = battn_tile_shape(a, r, CH);
         kvh = (int)battn_divide(at - before, f.total());
         before += kvh * f.total();
         int lo = 0, hi = f.tiles;
@@ -206,7 +209,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
         kb = (const bf16_t *)a.k;
         vb = (const bf16_t *)a.v;
         if constexpr (PAGED) {
-            const long long cost = f.step + min((long long)(tile + 1) * BT_PAIRS, f.pairs);
+            const long long cost = f.cost(tile);
             b0 = (int)battn_divide(at - before, block_cost);
             if (end < before + cost) b1 = (int)min((long long)n_blocks, battn_divide(end - before, block_cost));
             b1 = battn_same(b1);
@@ -366,13 +369,13 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
         bool goes_on = false;
         if constexpr (PAGED) {
             if (!whole && b0 == 0 && tid == 0)                // it goes on in the runs behind this one
-                ((FewMerge *)a.ws)[run] = FewMerge{battn_run_of(before + f.step + min((long long)(tile + 1) * BT_PAIRS, f.pairs) - 1, run_q, run_rem) - run + 1, r0, kvh,
+                ((FewMerge *)a.ws)[run] = FewMerge{battn_run_of(before + f.cost(tile) - 1, run_q, run_rem) - run + 1, r0, kvh,
                                                    tile * BT_PAIRS, (int)min((long long)BT_PAIRS, f.pairs - p0)};
         }
         const int slot = 2 * run + (b0 == 0);
         // on to the next tile: its first block is on its way while this one is written (the buffer that it goes to has been read by all)
         if constexpr (PAGED) {
-            before = battn_same(before + f.step + min((long long)(tile + 1) * BT_PAIRS, f.pairs));
+            before = battn_same(before + f.cost(tile));
             goes_on = before < end;
             if (goes_on) {
                 at = before;
@@ -382,7 +385,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
                         kvh = 0;
                         do {
                             if (++r >= a.n_requests) goes_on = false;     // (never: the run lies in some requests)
-                            else f = battn_tile_shape(a, r);
+                            else f = battn_tile_shape(a, r, CH);
                         } while (goes_on && f.tiles == 0);
                     }
                 }

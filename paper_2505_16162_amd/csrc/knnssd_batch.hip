@@ -136,7 +136,8 @@ static void launch_battn(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, in
     }
     if (PAGED && kv_dtype == KNNSSD_BF16) return launch_paged_bf16<HD>(a, dtype, most_rows, s);
     const int64_t items = (int64_t)a.n_rows * a.H;
-    hipLaunchKernelGGL((battn_row_kernel<HD, PAGED>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
+    if (items < BR_FULL) hipLaunchKernelGGL((battn_row_kernel<HD, PAGED, 4>), dim3((unsigned)items), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((battn_row_kernel<HD, PAGED, 1>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
 }
 
 extern "C" size_t knnssd_paged_attention_bytes(const knnssd_pages *p, int32_t n_heads, int32_t dtype) {
