@@ -304,7 +304,7 @@ int32_t knnssd_stream_next_domain(int32_t current, int32_t n_domains, double mix
  * One round of a batch: knnssd_page_plan (once), then for every block knnssd_paged_store and knnssd_paged_attention. Calls that
  * share tables, pages or a workspace have to be ordered (one stream, or events).                                       */
 #define KNNSSD_MAX_REQUESTS 4096
-#define KNNSSD_MAX_ROW_HEADS (1 << 25)      /* rows times query heads of one attention call */
+#define KNNSSD_MAX_ROW_HEADS (1 << 25)      /* rows times query heads of an attention call; a quarter of it: requests times heads, rows of a store */
 
 /* The keys and values of one block in pages. Position p of page g and kv head h begins at element
  * g*page_stride + h*head_stride + p*pos_stride of k_dev and of v_dev: [page][head][position][head_dim] and
@@ -361,7 +361,7 @@ int32_t knnssd_page_plan(const knnssd_page_tables *tables, const int32_t *cached
  * both in dtype, rows q_out_stride / k_out_stride elements apart; either may lie over the same heads of qkv_dev. Keys and values go to
  * page slot / page_size, position slot % page_size, in the cache's type. A row whose slot is negative or outside the cache, or whose position is
  * negative, is skipped: nothing is written for it. No two rows may have the same slot. dtype KNNSSD_BF16 over an fp32 cache is refused
- * (KNNSSD_EINVAL). n_heads may be 0 (KNNSSD_ERANGE if negative or n_rows < 1). Bases and strides as in knnssd_pages. */
+ * (KNNSSD_EINVAL). n_heads may be 0 (KNNSSD_ERANGE if negative, n_rows outside [1, KNNSSD_MAX_ROW_HEADS / 4], rope_base not positive and finite). Bases and strides as in knnssd_pages. */
 int32_t knnssd_paged_store(const knnssd_pages *pages, const void *qkv_dev, int32_t dtype, int64_t qkv_stride, int32_t n_rows,
                            int32_t n_heads, const int32_t *slots_dev, const int32_t *positions_dev, float rope_base,
                            void *q_out_dev, int64_t q_out_stride, void *k_out_dev, int64_t k_out_stride, void *hip_stream);
@@ -375,8 +375,8 @@ int32_t knnssd_paged_store(const knnssd_pages *pages, const void *qkv_dev, int32
  * if the caller has one, else 0; it only chooses the kernels. How the sums over a row are grouped follows the batch; the same call gives the
  * same bits. ws_dev: knnssd_paged_attention_bytes of the same pages, n_heads and dtype (0: not a supported shape), 256-byte aligned, of any
  * contents; nothing in it outlives a call.
- * KNNSSD_ESHAPE where n_heads is not a multiple of n_kv_heads, KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows < 1 or
- * n_rows * n_heads > KNNSSD_MAX_ROW_HEADS, table_width < 1 or a scale that is not finite. Lengths beyond 2^30 are taken as 2^30. */
+ * KNNSSD_ESHAPE where n_heads is not a multiple of n_kv_heads, KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows < 1,
+ * n_rows * n_heads > KNNSSD_MAX_ROW_HEADS, n_requests * n_heads > KNNSSD_MAX_ROW_HEADS / 4, table_width < 1 or a scale that is not finite. Lengths beyond 2^30 are taken as 2^30. */
 size_t knnssd_paged_attention_bytes(const knnssd_pages *pages, int32_t n_heads, int32_t dtype);
 int32_t knnssd_paged_attention(const knnssd_pages *pages, const int32_t *block_table_dev, int32_t table_width,
                                const int32_t *row_start_dev, const int32_t *kv_len_dev, int32_t n_requests,

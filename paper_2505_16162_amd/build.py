@@ -8,7 +8,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libknnssd.so")
-SOURCES = ["knnssd.hip", "knnssd_batch.hip"]     # compiled side by side; the kernels that place their own loads are all in the first
+SOURCES = ["knnssd.hip", "knnssd_batch.hip"]     # compiled side by side
 NO_SPILL_KERNELS = ["gemv_kernel", "gemm_mfma_kernel", "prefill_gemm_kernel", "prefill_thin_kernel", "prefill_attn_kernel"]     # mangled-name fragments of the kernels that must not spill
 
 
@@ -24,8 +24,8 @@ def build_library(verbose: bool = False) -> str:
     cmd += ["-Rpass-analysis=kernel-resource-usage"]
     if verbose:
         print(" ".join(cmd))
-    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(len(SOURCES) + 1) as pool:      # the assembly text is compiled beside the objects
-        text = pool.submit(assembly_text)
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(2 * len(SOURCES)) as pool:      # the assembly texts are compiled beside the objects
+        texts = [pool.submit(assembly_text, s) for s in SOURCES]
         objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
         procs = list(pool.map(lambda so: _run(cmd + ["-o", so[1], os.path.join(CSRC, so[0])]), zip(SOURCES, objects)))
         if all(p.returncode == 0 for p in procs):
@@ -47,7 +47,7 @@ def build_library(verbose: bool = False) -> str:
             os.remove(LIB)
             raise RuntimeError(f"{current} spills {m.group(1)} vector registers; its hand-placed loads forbid that")
     try:
-        assembly = text.result()
+        assembly = "\n".join(t.result() for t in texts)
     except Exception:
         os.remove(LIB)      # what has not been checked is not kept
         raise
@@ -59,13 +59,13 @@ def _run(cmd):
     return subprocess.run(cmd, check=False, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
 
 
-def assembly_text() -> str:
-    """The device code of the kernels that place their own loads as assembly text (a second compile)."""
+def assembly_text(source: str = SOURCES[0]) -> str:
+    """A source's device code as assembly text (a second compile)."""
     with tempfile.TemporaryDirectory() as tmp:
         asm = os.path.join(tmp, "knnssd.s")
         cmd = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-S", "--cuda-device-only",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument",
-               "-I", os.path.join(HERE, "..", "include"), "-o", asm, os.path.join(CSRC, SOURCES[0])]
+               "-I", os.path.join(HERE, "..", "include"), "-o", asm, os.path.join(CSRC, source)]
         proc = _run(cmd)
         if proc.returncode != 0:
             raise RuntimeError("hipcc -S failed:\n" + proc.stderr[-4000:])
@@ -76,7 +76,7 @@ def check_hand_placed_loads(text: str, verbose: bool = False) -> None:
     """The static checks of isa_check.py on the assembly text: the library is deleted and the
     build fails if the GEMV has any instruction that can touch a register with a hand-placed load in flight, if a
     variant of the verification GEMM copies or spills a register of its weight stream, or if m0 or the count of the
-    loads in flight is not what the prefill kernels' loads to LDS rely on."""
+    loads in flight is not what the prompt and batch kernels' loads to LDS rely on."""
     from . import isa_check
     problems = []
     gemv = isa_check.kernel_bodies(text, "gemv_kernel")
@@ -89,14 +89,14 @@ def check_hand_placed_loads(text: str, verbose: bool = False) -> None:
     for name, body in gemv + gemm:
         for n, t in isa_check.weight_register_copies(body)[:5]:
             problems.append(f"{name}: line {n}: {t}: reads a register of the weight stream")
-    prefill = [b for k in ("prefill_gemm_kernel", "prefill_thin_kernel", "prefill_attn_kernel") for b in isa_check.kernel_bodies(text, k)]
+    prefill = [b for k in ("prefill_gemm_kernel", "prefill_thin_kernel", "prefill_attn_kernel", "battn_tile_kernel") for b in isa_check.kernel_bodies(text, k)]
     if not prefill:
         problems.append("prefill kernels not found in the assembly text")
     for name, body in prefill:
         for n, t, why in isa_check.lds_load_flags(body)[:5]:
             problems.append(f"{name}: line {n}: {t}: {why}")
     if verbose:
-        print(f"isa_check: {len(gemv)} GEMV, {len(gemm)} GEMM and {len(prefill)} prefill kernel bodies, {len(problems)} problems")
+        print(f"isa_check: {len(gemv)} GEMV, {len(gemm)} GEMM and {len(prefill)} prompt and batch kernel bodies, {len(problems)} problems")
     if problems:
         os.remove(LIB)
         raise RuntimeError("hand-placed loads: the compiled code is not safe:\n" + "\n".join(problems))

@@ -58,7 +58,7 @@ extern "C" int32_t knnssd_paged_store(const knnssd_pages *p, const void *qkv_dev
     KS_TRY(pages_check(p));
     if (!qkv_dev || !slots_dev || !positions_dev) return KNNSSD_EINVAL;
     if (!dtype_ok(dtype) || !types_go_together(dtype, p->kv_dtype)) return KNNSSD_EINVAL;
-    if (n_rows < 1 || n_heads < 0 || n_heads > 65535 || !(rope_base > 0.f) || !std::isfinite(rope_base)) return KNNSSD_ERANGE;
+    if (n_rows < 1 || n_rows > KNNSSD_MAX_ROW_HEADS / 4 || n_heads < 0 || n_heads > 65535 || !(rope_base > 0.f) || !std::isfinite(rope_base)) return KNNSSD_ERANGE;
     const int64_t hd = p->head_dim;
     if (!rows_ok(qkv_dev, qkv_stride, (n_heads + 2 * (int64_t)p->n_kv_heads) * hd, dtype)) return KNNSSD_EINVAL;
     if (q_out_dev && !rows_ok(q_out_dev, q_out_stride, n_heads * hd, dtype)) return KNNSSD_EINVAL;
@@ -81,7 +81,7 @@ static int32_t rows_check(const int32_t *row_start_dev, int32_t n_requests, cons
     if (!row_start_dev || !q || !out || !dtype_ok(dtype)) return KNNSSD_EINVAL;
     if (n_requests < 1 || n_requests > KNNSSD_MAX_REQUESTS || n_rows < 1 || !std::isfinite(scale)) return KNNSSD_ERANGE;
     if (n_heads < 1 || n_heads > 65535 || n_heads % n_kv_heads) return KNNSSD_ESHAPE;
-    if ((int64_t)n_rows * n_heads > KNNSSD_MAX_ROW_HEADS) return KNNSSD_ERANGE;
+    if ((int64_t)n_rows * n_heads > KNNSSD_MAX_ROW_HEADS || (int64_t)n_requests * n_heads > KNNSSD_MAX_ROW_HEADS / 4) return KNNSSD_ERANGE;
     if (!rows_ok(q, q_stride, n_heads * hd, dtype) || !rows_ok(out, out_stride, n_heads * hd, dtype)) return KNNSSD_EINVAL;
     return KNNSSD_OK;
 }

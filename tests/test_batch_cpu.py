@@ -25,7 +25,7 @@ def pages(**kw):
 BAD_PAGES = [(dict(k_dev=None), EINVAL), (dict(v_dev=None), EINVAL), (dict(k_dev=A + 8), EINVAL), (dict(v_dev=A + 2), EINVAL), (dict(kv_dtype=2), EINVAL),
              (dict(head_dim=80), ESHAPE), (dict(head_dim=256), ESHAPE), (dict(n_kv_heads=0), ESHAPE), (dict(page_size=4), ESHAPE), (dict(page_size=24), ESHAPE),
              (dict(page_size=2048), ESHAPE), (dict(n_pages=0), ESHAPE), (dict(n_pages=2 ** 27, page_size=16), ESHAPE), (dict(pos_stride=120), EINVAL),
-             (dict(pos_stride=129), EINVAL), (dict(head_stride=64), EINVAL), (dict(head_stride=16 * 128 + 4), EINVAL), (dict(page_stride=-4096), EINVAL)]
+             (dict(pos_stride=129), EINVAL), (dict(head_stride=64), EINVAL), (dict(pos_stride=2 ** 26 + 8), ESHAPE), (dict(head_stride=16 * 128 + 4), EINVAL), (dict(page_stride=-4096), EINVAL)]
 
 
 def attention(lib, p, **kw):
@@ -53,7 +53,8 @@ def test_pages(lib, kw, code):
     (dict(table=None), EINVAL), (dict(row_start=None), EINVAL), (dict(kv_len=None), EINVAL), (dict(q=None), EINVAL), (dict(out=None), EINVAL), (dict(ws=None), EINVAL),
     (dict(ws=A + 16), EINVAL), (dict(wsb=0), EINVAL), (dict(q=A + 8), EINVAL), (dict(out=A + 4), EINVAL), (dict(qs=4 * 128 - 8), EINVAL), (dict(os=4 * 128 + 4), EINVAL),
     (dict(qs=-1024), EINVAL), (dict(dtype=3), EINVAL), (dict(n=0), ERANGE), (dict(n=4097), ERANGE), (dict(rows=0), ERANGE), (dict(width=0), ERANGE), (dict(most=-1), ERANGE),
-    (dict(scale=float("nan")), ERANGE), (dict(scale=float("inf")), ERANGE), (dict(heads=3), ESHAPE), (dict(heads=0), ESHAPE)])
+    (dict(scale=float("nan")), ERANGE), (dict(scale=float("inf")), ERANGE), (dict(heads=3), ESHAPE), (dict(heads=0), ESHAPE),
+    (dict(rows=2 ** 23 + 1), ERANGE), (dict(n=4096, heads=4096, qs=4096 * 128, os=4096 * 128), ERANGE)])
 def test_paged_attention(lib, kw, code):
     assert attention(lib, pages(), **kw) == code
 
@@ -72,7 +73,7 @@ def test_types_that_do_not_go_together(lib):
 
 @pytest.mark.parametrize("kw,code", [
     (dict(qkv=None), EINVAL), (dict(slots=None), EINVAL), (dict(positions=None), EINVAL), (dict(qkv=A + 8), EINVAL), (dict(dtype=2), EINVAL), (dict(qs=7 * 128), EINVAL),
-    (dict(rows=0), ERANGE), (dict(heads=-1), ERANGE), (dict(base=0.0), ERANGE), (dict(base=float("inf")), ERANGE), (dict(base=float("nan")), ERANGE),
+    (dict(rows=0), ERANGE), (dict(rows=2 ** 23 + 1), ERANGE), (dict(heads=-1), ERANGE), (dict(base=0.0), ERANGE), (dict(base=float("inf")), ERANGE), (dict(base=float("nan")), ERANGE),
     (dict(q_out=A + 2, qos=512), EINVAL), (dict(q_out=A, qos=511), EINVAL), (dict(k_out=A, kos=128), EINVAL)])
 def test_store(lib, kw, code):
     assert store(lib, pages(), **kw) == code

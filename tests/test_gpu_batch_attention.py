@@ -191,3 +191,64 @@ def test_two_streams():
     for c in cases:
         want, err = c.want(c.dim ** -0.5, BF16)
         B.check_rows(c.out, want, err, BF16)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+def test_values_that_are_not_finite_in_places_that_no_row_sees(types):
+    """A request of no rows whose cache holds NaN, page tails and pages of nobody (NaN in every case here), and a table whose ids lie outside the cache."""
+    c = B.PagedCase([2, 0, 1], [40, 60, 33], 4, 2, 64, 16, *types)
+    for j in range(4):
+        c.k_pages[c.table[1, j]] = math.nan
+        c.v_pages[c.table[1, j]] = math.inf
+    check_paged(c)
+    check_paged(c, most_rows=100)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+def test_tables_that_lie_point_somewhere_in_the_cache(types):
+    """Page ids outside the cache, lengths beyond the table, rows beyond the batch: wrong values, never an access out of range."""
+    c = B.PagedCase([3, 40], [100, 90], 4, 2, 64, 16, *types)
+    good = run_paged(c, most_rows=40).clone()
+    table, lens, start = c.block_table.clone(), c.kv_len.clone(), c.row_start.clone()
+    for bad in (-1, 2 ** 31 - 1, -2 ** 31, c.k_pages.shape[0]):
+        c.block_table[0].fill_(bad)
+        run_paged(c)
+    c.block_table.copy_(table)
+    for bad in (2 ** 31 - 1, -5, -2 ** 31):
+        c.kv_len[0] = bad
+        run_paged(c)
+    c.kv_len.copy_(lens)
+    for bad in ([0, 2 ** 31 - 1, 43], [0, 3, 2 ** 31 - 1], [-7, 3, 43], [5, 3, 43], [0, -9, 43], [0, 0, 0]):
+        c.row_start.copy_(torch.tensor(bad, dtype=torch.int32))
+        run_paged(c)
+        binding.knnssd_prompt_attention(c.q, c.q[:, :2], c.q[:, 2:], c.row_start, out=c.out)
+    c.row_start.copy_(start)
+    c.out.fill_(5.0)
+    assert torch.equal(run_paged(c, most_rows=40), good)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+def test_many_requests(types):
+    """More requests than a wavefront looks at once (64), most of them without rows."""
+    rows = [0] * 300
+    for i, n in ((0, 2), (63, 1), (64, 3), (130, 20), (299, 1)):
+        rows[i] = n
+    lens = [r + (7 * i) % 50 for i, r in enumerate(rows)]
+    c = B.PagedCase(rows, lens, 4, 2, 64, 8, *types)
+    check_paged(c, most_rows=3 if types[0] == F32 else 0)
+    check_paged(c, most_rows=20)
+
+
+def test_scores_that_leave_the_first_block_far_behind():
+    """Tiles weigh against the first block's largest score: later ones 2^64 and more above it make the reference follow, in rows of their own."""
+    c = B.PagedCase([40, 3], [500, 200], 4, 2, 64, 16, BF16, BF16)
+    for r in range(2):
+        up = torch.ones(c.lens[r], 1, 1)
+        up[70:] = 40.0                                        # scores up to 40 times as large from here on, and again behind 300
+        up[300:] = 400.0
+        c.k[r] = (c.k[r].float() * up).to(BF16)
+        for j in range(-(-c.lens[r] // 16)):
+            m = min(16, c.lens[r] - j * 16)
+            c.k_pages[c.table[r, j], :, :m] = c.k[r][j * 16:j * 16 + m].permute(1, 0, 2).cuda()
+    check_paged(c)
+    check_paged(c, scale=1.0)
