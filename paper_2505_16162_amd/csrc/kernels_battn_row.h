@@ -4,25 +4,24 @@
 
 namespace ks {
 
-// A (row, head) at a time, in fp32 from end to end: the lanes that share a position take eight dimensions each, 64 / (HD / 8) positions at a time, four such
-// steps under way; each such group of lanes keeps its own running maximum and sum, merged at the end. W wavefronts share an item's positions: four where the items
-// are too few to fill the chip with one each (34 requests of up to 8 rows, 5 heads, 100 to 350 positions: 59 -> 19 us with both).
-// Bound by memory latency and by the exchanges between lanes; keys and values are read once for every row and head, from the caches.
-constexpr int BR_FULL = 4096;                                 // items from which a wavefront takes one alone
+// A (row, head) at a time, in fp32 from end to end, for the smallest calls: the lanes that share a position take eight dimensions each, 64 / (HD / 8) positions
+// at a time, four such steps under way; each such group of lanes keeps its own running maximum and sum, merged at the end, and the four
+// wavefronts of a workgroup share the item's positions. Bound by memory latency; keys and values are read once for every row and head, from the caches
+// (34 requests of up to 8 rows, 5 heads, 100 to 350 positions: 19 us; with one wavefront and one step at a time 59).
+constexpr int BR_FULL = 4096;                                 // (row, head) items from which the tiles are taken instead
 
-template <int HD, bool PAGED, int W>
+template <int HD, bool PAGED>
 __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
-    constexpr int LP = HD / 8, NP = 64 / LP, U = 4;
+    constexpr int LP = HD / 8, NP = 64 / LP, U = 4, W = 4;
     __shared__ float part[4][HD + 2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long long item = W == 1 ? (long long)blockIdx.x * 4 + wave : blockIdx.x;
-    const int t = (int)(item / a.H), h = (int)(item % a.H), kvh = h / a.group;
-    if (t >= a.n_rows || t >= a.row_start[a.n_requests]) return;      // (W = 4: the whole workgroup)
+    const int t = blockIdx.x / a.H, h = blockIdx.x % a.H, kvh = h / a.group;
+    if (t >= a.n_rows || t >= a.row_start[a.n_requests]) return;      // the whole workgroup
     const int r = battn_request(a.row_start, a.n_requests, t), r0 = max(a.row_start[r], 0);
     const int n = a.row_start[r + 1] - r0;
     const int len = PAGED ? battn_len(a, r) : n;
     const int last = PAGED ? min(len - n + (t - r0), len - 1) : t - r0;      // the row's own position
-    const int d = (lane % LP) * 8, sub = lane / LP + (W == 1 ? 0 : wave * NP);
+    const int d = (lane % LP) * 8, sub = lane / LP + wave * NP;
     float q[8], o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const float *qp = (const float *)a.q + t * a.q_stride + h * HD + d;
 #pragma unroll
@@ -80,25 +79,23 @@ __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = o[e] * f + lane_xor(o[e], off) * f2;
     }
-    if constexpr (W == 4) {
-        if (lane < LP) {
+    if (lane < LP) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) part[wave][d + e] = o[e];
-            if (lane == 0) { part[wave][HD] = m; part[wave][HD + 1] = l; }
-        }
-        __syncthreads();
-        if (wave != 0) return;
-        m = fmaxf(fmaxf(part[0][HD], part[1][HD]), fmaxf(part[2][HD], part[3][HD]));
-        l = 0.f;
+        for (int e = 0; e < 8; ++e) part[wave][d + e] = o[e];
+        if (lane == 0) { part[wave][HD] = m; part[wave][HD + 1] = l; }
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    m = fmaxf(fmaxf(part[0][HD], part[1][HD]), fmaxf(part[2][HD], part[3][HD]));
+    l = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = 0.f;
+    for (int e = 0; e < 8; ++e) o[e] = 0.f;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const float f = part[x][HD] == -INFINITY ? 0.f : exp2f(part[x][HD] - m);
-            l = fmaf(part[x][HD + 1], f, l);
+    for (int x = 0; x < 4; ++x) {
+        const float f = part[x][HD] == -INFINITY ? 0.f : exp2f(part[x][HD] - m);
+        l = fmaf(part[x][HD + 1], f, l);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = fmaf(part[x][d + e], f, o[e]);
-        }
+        for (int e = 0; e < 8; ++e) o[e] = fmaf(part[x][d + e], f, o[e]);
     }
     if (lane < LP) {
         const float inv = l > 0.f ? 1.f / l : 0.f;

@@ -1,4 +1,4 @@
-// Attention of a batch's many rows in bf16: over pages (PAGED) or over their own prompts' rows.
+// Attention of a batch's rows on the matrix cores: over pages (PAGED) or over their own prompts' rows.
 #pragma once
 #include <cfloat>
 #include <climits>
@@ -8,7 +8,7 @@
 namespace ks {
 
 // ------------------------------------------------------------------------------------------
-// Many rows, bf16: tiles of 128 (row, head) pairs of one kv head, 32 per wavefront, on the matrix cores.
+// Many rows: tiles of 128 (row, head) pairs of one kv head, 32 per wavefront, on the matrix cores.
 // Everything is computed transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane keeps one pair from the scores to the output: the
 // accumulators of S^T (position 8(i/4) + 4(lane/32) + i%4 of pair lane%32 in register i) are, rounded and packed as they lie, the operand of the
 // second product, whose other operand takes the values' positions in the same order by transposing reads of LDS. Nothing is
@@ -18,7 +18,7 @@ namespace ks {
 constexpr int BT_PAIRS = 128;
 // positions of a block: 64, or 32 over prompts in heads of 128, where the registers of a block's scores then leave room for a third wavefront on each SIMD
 // (two prompts of 4096 rows 418 -> 400 us; over pages, whose wavefronts need more of them, 512 -> 522 us)
-template <int HD, bool PAGED> constexpr int battn_tile_positions() { return HD == 128 && !PAGED ? 32 : 64; }
+template <int HD, bool PAGED, int NP> constexpr int battn_tile_positions() { return NP == 0 ? 32 * 128 / HD : HD == 128 && !PAGED ? 32 : 64; }
 
 // Tile `index` of the batch: its request and its number in there; false behind the last. Every wavefront for itself, 64 requests at a time.
 __device__ __forceinline__ bool battn_find_tile(const BattnArgs &a, int index, int &r_out, int &tile_out, int &tiles_out) {
@@ -49,7 +49,7 @@ __device__ __forceinline__ bool battn_find_tile(const BattnArgs &a, int index, i
     return false;
 }
 
-template <int HD, bool PAGED> constexpr int battn_tile_lds() { return 2 * 2 * battn_tile_positions<HD, PAGED>() * HD * 2; }
+template <int HD, bool PAGED, int NP> constexpr int battn_tile_lds() { return 2 * 2 * battn_tile_positions<HD, PAGED, NP>() * HD * (NP == 0 ? 4 : 2); }
 
 // Over pages the batch's tiles are dealt to the workgroups in equal runs, as in battn_few_kernel, by their cost: a tile's is the positions before its request's
 // new rows times the heads of a group, and the pairs up to its own last one (a pair's rows counted exactly), or a block's cost, positions of a block times heads
@@ -77,11 +77,12 @@ __device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r,
     return f;
 }
 
-// NP = 3: fp32 queries over a bf16 cache, which stay exact as three bf16 planes, as do the weights.
+// NP: 1 all in bf16; 3 fp32 queries over a bf16 cache, which stay exact as three bf16 planes, as do the weights; 0 all in fp32, on the fp32 matrix
+// instructions (two positions, or dimensions, each), which take keys, values and weights as they lie.
 template <int HD, bool PAGED, int NP>
-__global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_kernel(BattnArgs a) {
-    constexpr int KS = HD / 16, DT = HD / 32, SL = HD / 8, RB = HD * 2, MROW = HD + BF_PAD;
-    constexpr int CH = battn_tile_positions<HD, PAGED>(), KV = CH * RB;                             // bytes of a block's keys (or values)
+__global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void battn_tile_kernel(BattnArgs a) {
+    constexpr int KS = HD / 16, DT = HD / 32, ELT = NP == 0 ? 4 : 2, RB = HD * ELT, SL = RB / 16, MROW = HD + BF_PAD;
+    constexpr int CH = battn_tile_positions<HD, PAGED, NP>(), KV = CH * RB;                             // bytes of a block's keys (or values)
     constexpr int ROWS = 64 / SL, NI = KV / 1024 / 4;         // rows a wavefront's load covers, loads per wavefront for the keys
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -154,15 +155,15 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
     int buf = 0;                                              // where the next block goes
     // the segment: blocks [b0, b1) of a tile
     int r0, n, len, last, base, b0, b1, n_blocks;
-    const bf16_t *kb, *vb;
+    const char *kb, *vb;
     const_ints table;
     // first row of the wavefront's i-th load of block c (rows past the request's last repeat that one)
     auto load_row = [&](int c, int i) __attribute__((always_inline)) { return min(c * CH + (i * 4 + wave) * ROWS, last & -ROWS); };
     // order of a row's 16-byte pieces (exclusive or with these), so that LDS reads do not meet in one of its 64 banks: the keys' are 32 rows, two pieces of each,
-    // the values' four rows, four pieces of each, at a time
-    auto key_order = [](int row) { return HD == 128 ? row & 15 : (row >> 1) & 7; };
-    auto value_order = [](int row) { return HD == 128 ? (row & 3) << 2 : (row & 2) << 1; };
-    const int kpiece = (lane % SL) ^ key_order(wave * ROWS + lane / SL), vpiece = (lane % SL) ^ value_order(lane / SL);
+    // the values' four rows, four pieces of each, or (fp32) two rows four apart, eight pieces of each, at a time
+    auto key_order = [](int row) { return RB >= 256 ? row & 15 : (row >> 1) & 7; };
+    auto value_order = [](int row) { return NP == 0 ? (row & 4) << 1 : HD == 128 ? (row & 3) << 2 : (row & 2) << 1; };
+    const int kpiece = (lane % SL) ^ key_order(wave * ROWS + lane / SL), vpiece = (lane % SL) ^ value_order(wave * ROWS + lane / SL);
     int page[NI];
     auto look_up = [&](int c) __attribute__((always_inline)) {                               // the pages of block c
         if constexpr (PAGED)
@@ -174,27 +175,29 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
         for (int i = 0; i < NI; ++i) {
             const int b = load_row(c, i), in = min(lane / SL, last - b);
             const unsigned int d = l0 + buf * 2 * KV + (i * 4 + wave) * 1024;
+            const int kp = 16 * (kpiece ^ (key_order(i * 4 * ROWS) & 8));     // (eight rows a load of all wavefronts: every other one has the order's top bit)
             if constexpr (PAGED) {
                 const int pg = (unsigned)page[i] < (unsigned)a.n_pages ? page[i] : 0;
-                const long long at = pg * a.page_stride + (b & ((1 << a.shift) - 1)) * a.pos_stride;
-                const unsigned int off = (unsigned int)in * (unsigned int)a.pos_stride * 2u;
-                battn_dma(kb + at, off + kpiece * 16, d);
+                const long long at = (pg * a.page_stride + (b & ((1 << a.shift) - 1)) * a.pos_stride) * ELT;
+                const unsigned int off = (unsigned int)in * (unsigned int)a.pos_stride * ELT;
+                battn_dma(kb + at, off + kp, d);
                 battn_dma(vb + at, off + vpiece * 16, d + KV);
             } else {
-                battn_dma(kb + b * a.k_stride, (unsigned int)in * (unsigned int)a.k_stride * 2u + kpiece * 16, d);
-                battn_dma(vb + b * a.v_stride, (unsigned int)in * (unsigned int)a.v_stride * 2u + vpiece * 16, d + KV);
+                battn_dma(kb + b * a.k_stride * ELT, (unsigned int)in * (unsigned int)a.k_stride * ELT + kp, d);
+                battn_dma(vb + b * a.v_stride * ELT, (unsigned int)in * (unsigned int)a.v_stride * ELT + vpiece * 16, d + KV);
             }
         }
     };
     // where the lane reads in a block: keys of position col, dimensions 16 ks + 8 half ...; values of position 4 half + (lane % 16) / 4 (and 8 on), four
-    // dimensions from 32 dt + 16 (lane / 16 % 2) + 4 (lane % 4)
-    unsigned int k_at[KS], v_at[DT];
+    // dimensions from 32 dt + 16 (lane / 16 % 2) + 4 (lane % 4). fp32: dimensions 8 ks + 4 half ...; position 4 half, dimension 32 dt + col
+    constexpr int KR = NP == 0 ? HD / 8 : KS;                 // the lane's reads of a position's keys
+    unsigned int k_at[KR], v_at[DT];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) k_at[ks] = l0 + col * RB + (((2 * ks + half) ^ key_order(col)) * 16);
+    for (int ks = 0; ks < KR; ++ks) k_at[ks] = l0 + col * RB + (((2 * ks + half) ^ key_order(col)) * 16);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-        const int v_row = 4 * half + ((lane & 15) >> 2), v_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-        v_at[dt] = l0 + KV + v_row * RB + (((4 * dt + (v_col >> 3)) ^ value_order(v_row)) * 16) + (v_col & 4) * 2;
+        const int v_row = 4 * half + (NP == 0 ? 0 : (lane & 15) >> 2), v_col = NP == 0 ? col : 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+        v_at[dt] = l0 + KV + v_row * RB + (((32 * dt + v_col) * ELT / 16) ^ value_order(v_row)) * 16 + v_col * ELT % 16;
     }
     auto enter = [&]() __attribute__((always_inline)) {       // the segment of `tile` that begins at `at`
         r0 = max(a.row_start[r], 0);
@@ -206,19 +209,19 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
         n_blocks = (max(base, 0) + tile_last) / CH + 1;
         b0 = 0;
         b1 = n_blocks;
-        kb = (const bf16_t *)a.k;
-        vb = (const bf16_t *)a.v;
+        kb = (const char *)a.k;
+        vb = (const char *)a.v;
         if constexpr (PAGED) {
             const long long cost = f.cost(tile);
             b0 = (int)battn_divide(at - before, block_cost);
             if (end < before + cost) b1 = (int)min((long long)n_blocks, battn_divide(end - before, block_cost));
             b1 = battn_same(b1);
-            kb += kvh * a.head_stride;
-            vb += kvh * a.head_stride;
+            kb += kvh * a.head_stride * ELT;
+            vb += kvh * a.head_stride * ELT;
             table = a.table + (size_t)r * a.width;
         } else {
-            kb += (long long)r0 * a.k_stride + kvh * HD;
-            vb += (long long)r0 * a.v_stride + kvh * HD;
+            kb += ((long long)r0 * a.k_stride + kvh * HD) * ELT;
+            vb += ((long long)r0 * a.v_stride + kvh * HD) * ELT;
         }
         if (len > 0 && b0 < b1) {
             look_up(b0);
@@ -235,19 +238,25 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
         const bool live = p0 + wave * 32 + col < f.pairs;
         const int row = (int)(pair / a.group), g = (int)(pair - (long long)row * a.group);
         const int limit = base + row;                         // the lane's last visible position
-        bf16x8_t qf[KS][NP];                                  // dimensions 16 ks + 8 half ... of the lane's pair
+        bf16x8_t qf[KS][NP == 0 ? 1 : NP];                    // dimensions 16 ks + 8 half ... of the lane's pair
+        f32x4_t qs[NP == 0 ? KR : 1];                         // fp32: 8 ks + 4 half ...
         {
-            const long long q_at = (long long)(r0 + row) * a.q_stride + (kvh * a.group + g) * HD + half * 8;
+            const long long q_at = (long long)(r0 + row) * a.q_stride + (kvh * a.group + g) * HD + half * (NP == 0 ? 4 : 8);
+            if constexpr (NP == 0) {
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                if constexpr (NP == 1) {
-                    qf[ks][0] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + q_at + ks * 16) ^ (flip | flip >> 16));
-                } else {
-                    const u32x4_t lo = *reinterpret_cast<const u32x4_t *>((const float *)a.q + q_at + ks * 16) ^ flip, hi = *reinterpret_cast<const u32x4_t *>((const float *)a.q + q_at + ks * 16 + 4) ^ flip;
-                    float v[8];
+                for (int ks = 0; ks < KR; ++ks) qs[ks] = __builtin_bit_cast(f32x4_t, *reinterpret_cast<const u32x4_t *>((const float *)a.q + q_at + ks * 8) ^ flip);
+            } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) { v[e] = __uint_as_float(lo[e]); v[4 + e] = __uint_as_float(hi[e]); }
-                    battn_planes<3>(v, qf[ks]);
+                for (int ks = 0; ks < KS; ++ks) {
+                    if constexpr (NP == 1) {
+                        qf[ks][0] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>((const bf16_t *)a.q + q_at + ks * 16) ^ (flip | flip >> 16));
+                    } else {
+                        const u32x4_t lo = *reinterpret_cast<const u32x4_t *>((const float *)a.q + q_at + ks * 16) ^ flip, hi = *reinterpret_cast<const u32x4_t *>((const float *)a.q + q_at + ks * 16 + 4) ^ flip;
+                        float v[8];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { v[e] = __uint_as_float(lo[e]); v[4 + e] = __uint_as_float(hi[e]); }
+                        battn_planes<3>(v, qf[ks]);
+                    }
                 }
             }
         }
@@ -272,12 +281,17 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
+                for (int ks = 0; ks < KR; ++ks) {
                     unsigned int from = k_at[ks] + buf * 2 * KV;
                     asm("" : "+v"(from));                     // (one address, the tiles by the read's own offset)
-                    const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(__attribute__((address_space(3))) const u32x4_t *)(uintptr_t)(from + t * 32 * RB));
+                    const u32x4_t kf = *(__attribute__((address_space(3))) const u32x4_t *)(uintptr_t)(from + t * 32 * RB);
+                    if constexpr (NP == 0) {
 #pragma unroll
-                    for (int q = NP - 1; q >= 0; --q) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][q], s[t], 0, 0, 0);
+                        for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), qs[ks][e], s[t], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int q = NP - 1; q >= 0; --q) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), qf[ks][q], s[t], 0, 0, 0);
+                    }
                 }
             }
             if (c * CH + CH - 1 > base + wave_first) {  // some of the block's positions lie behind some of the wavefront's rows
@@ -335,19 +349,31 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED ? 3 : 2) void battn_tile_k
                 from[dt] = v_at[dt] + buf * 2 * KV;
                 asm("" : "+v"(from[dt]));
             }
+            if constexpr (NP == 0) {
 #pragma unroll
-            for (int st = 0; st < CH / 16; ++st) {                  // 16 positions
-                const int t = st >> 1, i0 = (st & 1) * 8;
-                const float pv[8] = {s[t][i0], s[t][i0 + 1], s[t][i0 + 2], s[t][i0 + 3], s[t][i0 + 4], s[t][i0 + 5], s[t][i0 + 6], s[t][i0 + 7]};
-                bf16x8_t pb[NP];
-                battn_planes<NP>(pv, pb);
+                for (int t = 0; t < CH / 32; ++t)
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)(from[dt] + st * 16 * RB));
-                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)(from[dt] + st * 16 * RB + 8 * RB));
-                    const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    for (int i = 0; i < 16; ++i)              // position 8 (i/4) + i%4 and four on: a weight is an operand as it lies
 #pragma unroll
-                    for (int q = NP - 1; q >= 0; --q) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[q], o[dt], 0, 0, 0);
+                        for (int dt = 0; dt < DT; ++dt) {
+                            const float vf = *(__attribute__((address_space(3))) const float *)(uintptr_t)(from[dt] + (t * 32 + 8 * (i / 4) + i % 4) * RB);
+                            o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[t][i], o[dt], 0, 0, 0);
+                        }
+            } else {
+#pragma unroll
+                for (int st = 0; st < CH / 16; ++st) {                  // 16 positions
+                    const int t = st >> 1, i0 = (st & 1) * 8;
+                    const float pv[8] = {s[t][i0], s[t][i0 + 1], s[t][i0 + 2], s[t][i0 + 3], s[t][i0 + 4], s[t][i0 + 5], s[t][i0 + 6], s[t][i0 + 7]};
+                    bf16x8_t pb[NP == 0 ? 1 : NP];
+                    battn_planes<NP>(pv, pb);
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)(from[dt] + st * 16 * RB));
+                        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)(from[dt] + st * 16 * RB + 8 * RB));
+                        const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                        for (int q = NP - 1; q >= 0; --q) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[q], o[dt], 0, 0, 0);
+                    }
                 }
             }
         };

@@ -98,8 +98,13 @@ static int64_t tiles_bound(const BattnArgs &a) { return (((int64_t)a.n_rows * a.
 
 template <int HD, int NP>
 static void launch_paged_tiles(const BattnArgs &a, int64_t most, hipStream_t s) {
-    hipLaunchKernelGGL((battn_tile_kernel<HD, true, NP>), dim3(BF_WGS), dim3(256), (battn_tile_lds<HD, true>()), s, a);
-    launch_merge<HD, NP>(a, BF_WGS, (int)(most < BT_PAIRS ? most : BT_PAIRS), tiles_bound(a), BT_PAIRS, s);
+    hipLaunchKernelGGL((battn_tile_kernel<HD, true, NP>), dim3(BF_WGS), dim3(256), (battn_tile_lds<HD, true, NP>()), s, a);
+    launch_merge<HD, NP == 1 ? 1 : 3>(a, BF_WGS, (int)(most < BT_PAIRS ? most : BT_PAIRS), tiles_bound(a), BT_PAIRS, s);
+}
+
+template <int HD, int NP>
+static void launch_prompt_tiles(const BattnArgs &a, hipStream_t s) {
+    hipLaunchKernelGGL((battn_tile_kernel<HD, false, NP>), dim3((unsigned)tiles_bound(a)), dim3(256), (battn_tile_lds<HD, false, NP>()), s, a);
 }
 
 // most (row, head) pairs of one kv head that a request may have for battn_few_kernel to take the batch
@@ -115,11 +120,17 @@ static void launch_few(const BattnArgs &a, int64_t most, hipStream_t s) {
     launch_merge<HD, NP>(a, runs, (int)(most < FEW_PAIRS ? most : FEW_PAIRS), groups * a.Hkv, FEW_PAIRS, s);
 }
 
-// attention over a bf16 cache
+// In fp32 the tiles' matrix instructions take 8000 cycles a block, however few pairs a tile has; few rows over short contexts are done sooner by battn_row_kernel
+// (three prompts of up to 45 rows, 4 heads: 5 us, in tiles 8.5; one row of 40 heads over 400 positions 17 and 23, over 1500 positions 52 and 24).
+static bool rows_alone(const BattnArgs &a, int64_t positions) { return (int64_t)a.n_rows * a.H < BR_FULL && positions <= 512; }
+
 template <int HD>
-static void launch_paged_bf16(const BattnArgs &a, int32_t dtype, int32_t most_rows, hipStream_t s) {
+static void launch_paged(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, int32_t most_rows, hipStream_t s) {
     const int64_t most = (int64_t)(most_rows > 0 && most_rows < a.n_rows ? most_rows : a.n_rows) * a.group;
-    if (most <= FEW_PAIRS) {
+    if (kv_dtype == KNNSSD_FP32) {
+        if (rows_alone(a, (int64_t)a.width << a.shift)) hipLaunchKernelGGL((battn_row_kernel<HD, true>), dim3((unsigned)(a.n_rows * a.H)), dim3(256), 0, s, a);
+        else launch_paged_tiles<HD, 0>(a, most, s);
+    } else if (most <= FEW_PAIRS) {
         if (dtype == KNNSSD_FP32) launch_few<HD, 3>(a, most, s);
         else launch_few<HD, 1>(a, most, s);
     } else {
@@ -128,22 +139,16 @@ static void launch_paged_bf16(const BattnArgs &a, int32_t dtype, int32_t most_ro
     }
 }
 
-template <int HD, bool PAGED>
-static void launch_battn(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, int32_t most_rows, hipStream_t s) {
-    if (!PAGED && dtype == KNNSSD_BF16) {
-        hipLaunchKernelGGL((battn_tile_kernel<HD, false, 1>), dim3((unsigned)tiles_bound(a)), dim3(256), (battn_tile_lds<HD, false>()), s, a);
-        return;
-    }
-    if (PAGED && kv_dtype == KNNSSD_BF16) return launch_paged_bf16<HD>(a, dtype, most_rows, s);
-    const int64_t items = (int64_t)a.n_rows * a.H;
-    if (items < BR_FULL) hipLaunchKernelGGL((battn_row_kernel<HD, PAGED, 4>), dim3((unsigned)items), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((battn_row_kernel<HD, PAGED, 1>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
+template <int HD>
+static void launch_prompts(const BattnArgs &a, int32_t dtype, hipStream_t s) {
+    if (dtype == KNNSSD_BF16) launch_prompt_tiles<HD, 1>(a, s);
+    else if (rows_alone(a, a.n_rows)) hipLaunchKernelGGL((battn_row_kernel<HD, false>), dim3((unsigned)(a.n_rows * a.H)), dim3(256), 0, s, a);
+    else launch_prompt_tiles<HD, 0>(a, s);
 }
 
 extern "C" size_t knnssd_paged_attention_bytes(const knnssd_pages *p, int32_t n_heads, int32_t dtype) {
     if (pages_check(p) != KNNSSD_OK || !dtype_ok(dtype) || !types_go_together(dtype, p->kv_dtype)) return 0;
     if (n_heads < 1 || n_heads > 65535 || n_heads % p->n_kv_heads) return 0;
-    if (p->kv_dtype == KNNSSD_FP32) return 256;
     const size_t slot = p->head_dim == 128 ? battn_few_slot<128>(BT_PAIRS) : battn_few_slot<64>(BT_PAIRS);
     return battn_few_merges() + 2 * BF_WGS * slot * sizeof(float);
 }
@@ -166,8 +171,8 @@ extern "C" int32_t knnssd_paged_attention(const knnssd_pages *p, const int32_t *
     a.H = n_heads; a.Hkv = p->n_kv_heads; a.group = n_heads / p->n_kv_heads;
     a.scale2 = scale * 1.4426950408889634f;
     a.ws = ws_dev;
-    if (p->head_dim == 128) launch_battn<128, true>(a, dtype, p->kv_dtype, most_rows, (hipStream_t)hip_stream);
-    else launch_battn<64, true>(a, dtype, p->kv_dtype, most_rows, (hipStream_t)hip_stream);
+    if (p->head_dim == 128) launch_paged<128>(a, dtype, p->kv_dtype, most_rows, (hipStream_t)hip_stream);
+    else launch_paged<64>(a, dtype, p->kv_dtype, most_rows, (hipStream_t)hip_stream);
     HIP_TRY(hipGetLastError());
     return KNNSSD_OK;
 }
@@ -186,8 +191,8 @@ extern "C" int32_t knnssd_prompt_attention(const void *q_dev, int64_t q_stride, 
     a.row_start = (const_ints)(uintptr_t)row_start_dev; a.n_requests = n_requests; a.n_rows = n_rows;
     a.H = n_heads; a.Hkv = n_kv_heads; a.group = n_heads / n_kv_heads;
     a.scale2 = scale * 1.4426950408889634f;
-    if (head_dim == 128) launch_battn<128, false>(a, dtype, dtype, 0, (hipStream_t)hip_stream);
-    else launch_battn<64, false>(a, dtype, dtype, 0, (hipStream_t)hip_stream);
+    if (head_dim == 128) launch_prompts<128>(a, dtype, (hipStream_t)hip_stream);
+    else launch_prompts<64>(a, dtype, (hipStream_t)hip_stream);
     HIP_TRY(hipGetLastError());
     return KNNSSD_OK;
 }

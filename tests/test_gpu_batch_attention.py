@@ -252,3 +252,23 @@ def test_scores_that_leave_the_first_block_far_behind():
             c.k_pages[c.table[r, j], :, :m] = c.k[r][j * 16:j * 16 + m].permute(1, 0, 2).cuda()
     check_paged(c)
     check_paged(c, scale=1.0)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(40, 40, 128), (10, 2, 64), (8, 8, 64)])
+def test_fp32_on_the_matrix_cores(heads, kv_heads, dim):
+    """Enough rows, or a long enough table, for the tiles in fp32: prompts, chunks and single rows."""
+    check_paged(B.PagedCase([120, 1, 300 if dim == 64 else 30], [500, 2300, 301], heads, kv_heads, dim, 32, F32, F32), most_rows=300)
+    check_paged(B.PagedCase([1, 5], [2500, 70], heads, kv_heads, dim, 16, F32, F32, order="position"), most_rows=5)
+    g = torch.Generator().manual_seed(dim)
+    lens = [0, 130, 1, 300 if dim == 64 else 64, 33]
+    start = [sum(lens[:i]) for i in range(len(lens) + 1)]
+    qkv = torch.randn(start[-1] + 60, heads + 2 * kv_heads, dim, generator=g)
+    qkv[start[-1]:] = math.nan
+    n_rows = max(qkv.shape[0], 4200 // heads)
+    qkv = torch.cat([qkv, torch.full((n_rows - qkv.shape[0] + 1, *qkv.shape[1:]), math.nan)])
+    out = torch.full((qkv.shape[0], heads, dim), 5.0, device="cuda")
+    q, k, v = qkv.cuda().split([heads, kv_heads, kv_heads], 1)
+    binding.knnssd_prompt_attention(q, k, v, torch.tensor(start, dtype=torch.int32, device="cuda"), out=out)
+    q, k, v = qkv.split([heads, kv_heads, kv_heads], 1)
+    both = [B.attend64(q[a:b], k[a:b], v[a:b], dim ** -0.5) for a, b in zip(start, start[1:])]
+    B.check_rows(out, torch.cat([o for o, _ in both]), torch.cat([e for _, e in both]), F32)
