@@ -342,6 +342,7 @@ typedef struct knnssd_batch_rows {
  * pages: those it no longer needs (rejected drafts, a finished request with cached = added = 0) go back to the stack and their
  * table entries become -1, then those it lacks are taken. The order is fixed: pages go back in descending order of request
  * and page and are taken in ascending order, so the same state and lengths give the same tables.
+ * cached_dev or added_dev may be kv_len_dev itself (the lengths of the last round, all 0 after a round that could not be done).
  * result_dev[2] says in stream order whether it could be done: KNNSSD_PLAN_OK, or one of the following, the first that holds, and then tables and
  * stack are as they were, row_start and kv_len all 0, slots and positions all -1: the rest of the round does nothing.
  * KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS] or max_rows < 1, KNNSSD_ESHAPE for a page size or pool outside what knnssd_pages

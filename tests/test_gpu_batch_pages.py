@@ -47,6 +47,26 @@ def test_rounds_of_a_batch(n, page, most, max_rows):
         cached = [0 if rng.random() < 0.2 else c + rng.randint(0, a) for c, a in zip(cached, added)]
 
 
+@pytest.mark.parametrize("n,max_rows", [(5, 100), (300, 1500), (2000, 9000)])
+def test_lengths_over_the_arrays_of_the_last_round(n, max_rows):
+    """cached (then added) is the round's own kv_len: the plan overwrites its own argument."""
+    rng = random.Random(n)
+    stack, tables, rows = B.Stack(n, 8, 6 * n, 8), binding.PageTables.fresh(n, 64, 6 * n, 8), binding.BatchRows(n, max_rows)
+    cached = [0] * n
+    rows.kv_len.zero_()
+    for _ in range(8):
+        added = [rng.randint(0, 4) for _ in range(n)]
+        want = stack.plan(cached, added, max_rows)
+        binding.knnssd_page_plan(tables, rows, rows.kv_len, ints(added))
+        same(stack, tables, want, rows)
+        cached = want["kv_len"]
+    added = [rng.randint(0, 4) for _ in range(n)]
+    rows.kv_len.copy_(ints(added))
+    want = stack.plan([9] * n, added, max_rows)
+    binding.knnssd_page_plan(tables, rows, ints([9] * n), rows.kv_len)
+    same(stack, tables, want, rows)
+
+
 def test_the_largest_batch_whose_last_request_has_all_rows():
     n = 4096
     stack, tables, rows = B.Stack(n, 5, 9, 8), binding.PageTables.fresh(n, 40, 9, 8), binding.BatchRows(n, 40)
