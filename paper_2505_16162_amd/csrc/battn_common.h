@@ -171,6 +171,7 @@ __global__ __launch_bounds__(BM_NT) void battn_merge_kernel(BattnArgs a, int slo
             for (int u = 0; u < U; ++u) {
                 const int y = x + subs * u;
                 at[u] = -INFINITY;
+                l[u] = 0.f;
                 if (y < m.runs) {
                     const float *from = first + (2 * y + (y == 0)) * slot;
                     at[u] = from[HD];
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(BM_NT) void battn_merge_kernel(BattnArgs a, int slo
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (at[u] == -INFINITY) continue;
+                if (l[u] == 0.f) continue;                    // nothing seen (what was seen has a weight of 1 at least, or is NaN)
                 const float now = fmaxf(top, at[u]), k0 = __builtin_amdgcn_exp2f(top - now), k1 = __builtin_amdgcn_exp2f(at[u] - now);
                 top = now;
                 sum = sum * k0 + l[u] * k1;

@@ -205,6 +205,41 @@ def test_values_that_are_not_finite_in_places_that_no_row_sees(types):
 
 
 @pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("rows,lens", [([3, 1, 2], [900, 40, 700]), ([60, 30], [900, 200]), ([2, 3], [30, 40])])
+def test_not_a_number_stays_in_the_rows_that_see_it(rows, lens, types):
+    """A query, and a key that all rows of a request see: their outputs are NaN, all others as without."""
+    c = B.PagedCase(rows, lens, 4, 2, 64, 16, *types)
+    good = run_paged(c, most_rows=max(rows)).clone()
+    c.q[0, 1] = math.nan                                      # row 0, head 1
+    c.k_pages[c.table[1, 0], 1, 3] = math.nan                 # request 1, kv head 1
+    c.out.fill_(5.0)
+    got = run_paged(c, most_rows=max(rows))
+    lost = torch.zeros(got.shape[:2], dtype=torch.bool)
+    lost[0, 1] = True
+    lost[c.start[1]:c.start[2], 2:] = True
+    assert torch.isnan(got[lost]).all()
+    assert torch.equal(got[~lost], good[~lost])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [[5, 9], [300, 170]])
+def test_not_a_number_in_a_prompt(rows, dtype):
+    """A query's is its own row's; a key's is that of its own row and the later ones of its request."""
+    g = torch.Generator().manual_seed(9)
+    start = torch.tensor([0, rows[0], sum(rows)], dtype=torch.int32, device="cuda")
+    q, k, v = (torch.randn(sum(rows), h, 64, generator=g).to(dtype).cuda() for h in (4, 2, 2))
+    good = binding.knnssd_prompt_attention(q, k, v, start).clone()
+    q[1, 1] = math.nan
+    k[rows[0] + 4, 1] = math.nan
+    got = binding.knnssd_prompt_attention(q, k, v, start)
+    lost = torch.zeros(got.shape[:2], dtype=torch.bool)
+    lost[1, 1] = True
+    lost[rows[0] + 4:, 2:] = True
+    assert torch.isnan(got[lost]).all()
+    assert torch.equal(got[~lost], good[~lost])
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
 def test_tables_that_lie_point_somewhere_in_the_cache(types):
     """Page ids outside the cache, lengths beyond the table, rows beyond the batch: wrong values, never an access out of range."""
     c = B.PagedCase([3, 40], [100, 90], 4, 2, 64, 16, *types)
