@@ -1,7 +1,6 @@
 // Host side of the batch calls of the C ABI: page plans, rotary store into pages, attention over pages and over prompts.
 #include <hip/hip_runtime.h>
 
-#include <climits>
 #include <cmath>
 
 #include "hip_try.h"
@@ -107,7 +106,9 @@ static void launch_prompt_tiles(const BattnArgs &a, hipStream_t s) {
     hipLaunchKernelGGL((battn_tile_kernel<HD, false, NP>), dim3((unsigned)tiles_bound(a)), dim3(256), (battn_tile_lds<HD, false, NP>()), s, a);
 }
 
-// most (row, head) pairs of one kv head that a request may have for battn_few_kernel to take the batch
+// Most (row, head) pairs of one kv head that a request may have for battn_few_kernel to take the batch: as many as one group holds. 40 heads over 8: 32 requests of
+// one to three rows at 200 to 4000 positions take 61 us, in tiles 66, a single row 9.5 and 14; 20 to 30 pairs, two groups that each read the cache (two requests at 100 000 positions),
+// 159 and 145; 33 to 60 pairs 84 to 195 and 76 to 148.
 static const int FEW_PAIRS = 16;
 
 template <int HD, int NP>
