@@ -16,7 +16,7 @@ namespace ks {
 // Keys and values come in blocks of 32 or 64 positions straight to LDS, one block ahead.
 // What bounds it: over prompts and chunks the vector unit (exponentials, packing) beside the matrix cores, which do not wait for one another within a wavefront but do
 // between two products of one; two or three wavefronts on a SIMD fill that partly. Two prompts of 4096 rows, 40 heads of 128, bf16: 366 us = 938 TFLOP/s (matrix cores busy
-// 51 % of the time, the vector unit as much); eight chunks of up to 900 rows over 700 to 9000 positions in pages, 40 heads over 8: 492 us = 770 TFLOP/s. In fp32 the matrix instructions
+// 51 % of the time, the vector unit as much; on zeros, where the power limit leaves more clock, a quarter faster); eight chunks of up to 900 rows over 700 to 9000 positions in pages, 40 heads over 8: 492 us = 770 TFLOP/s. In fp32 the matrix instructions
 // themselves: a sixteenth of the bf16 rate.
 // ------------------------------------------------------------------------------------------
 constexpr int BT_PAIRS = 128;
