@@ -307,3 +307,35 @@ def test_fp32_on_the_matrix_cores(heads, kv_heads, dim):
     q, k, v = qkv.split([heads, kv_heads, kv_heads], 1)
     both = [B.attend64(q[a:b], k[a:b], v[a:b], dim ** -0.5) for a, b in zip(start, start[1:])]
     B.check_rows(out, torch.cat([o for o, _ in both]), torch.cat([e for _, e in both]), F32)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_group_of_more_heads_than_a_tile_has_pairs(dim, types):
+    """200 query heads of one kv head: a row's heads lie in two or three tiles, 13 groups of 16."""
+    check_paged(B.PagedCase([2, 0, 3, 1], [70, 5, 3, 300], 200, 1, dim, 16, *types))
+    check_paged(B.PagedCase([1], [90], 200, 1, dim, 16, *types), most_rows=1)
+    if types[0] == types[1]:
+        g = torch.Generator().manual_seed(3)
+        q, k, v = (torch.randn(35, h, dim, generator=g).to(types[0]) for h in (200, 1, 1))
+        out = binding.knnssd_prompt_attention(q.cuda(), k.cuda(), v.cuda(), torch.tensor([0, 2, 35], dtype=torch.int32, device="cuda"))
+        both = [B.attend64(q[a:b], k[a:b], v[a:b], dim ** -0.5, BF16 if types[0] == BF16 else None) for a, b in ((0, 2), (2, 35))]
+        B.check_rows(out, torch.cat([o for o, _ in both]), torch.cat([e for _, e in both]), types[0])
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+def test_the_most_requests_of_a_call(types):
+    """4096 requests, over pages with and without a bound of their rows, and as prompts of no row or one."""
+    rows = [1] * 4090 + [0, 0, 2, 0, 0, 3]
+    lens = [a + (7 * i) % 30 for i, a in enumerate(rows)]
+    c = B.PagedCase(rows, lens, 2, 1, 64, 8, *types)
+    want, err = c.want(0.125, BF16 if types[0] == BF16 else None)
+    for most in (3, 0):
+        c.out.fill_(5.0)
+        B.check_rows(run_paged(c, most_rows=most), want, err, types[0])
+    if types[0] == types[1]:
+        out = binding.knnssd_prompt_attention(c.q[:4090], c.q[:4090, :1], c.q[:4090, 1:], c.row_start)
+        # One row a request: its own value v, as (w v) (1 / w) with a weight w that the score's product and sum leave within some steps of 1. Three
+        # roundings, the product's, the reciprocal's and their product's, of half a step each: (1 + e)^3 - 1 < 4 e. Rounded to bf16 that is v.
+        own = c.q[:4090, 1:].expand(-1, 2, -1)
+        assert ((out - own).abs() <= (0 if types[0] == BF16 else 4 * B.EPS32) * own.abs()).all()
