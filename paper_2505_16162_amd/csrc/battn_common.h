@@ -3,6 +3,7 @@
 #include <type_traits>
 
 #include "kernels_pages.h"
+#include "rows_range.h"
 
 namespace ks {
 

@@ -24,7 +24,7 @@ template <int HD> __host__ __device__ constexpr int battn_few_positions() { retu
 struct FewShape { int n, blocks, pair_groups; };
 __device__ __forceinline__ FewShape battn_few_shape(const BattnArgs &a, int r, int group_pairs, int positions) {
     FewShape f{0, 1, 0};
-    const int n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
+    const int n = rows_of(a.row_start, r, a.n_rows).n;
     if (n > 0) {
         f.n = n;
         f.blocks = max(1, (battn_len(a, r) + positions - 1) / positions);
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
         b1 = battn_same((int)min((long long)f.blocks, b0 + (unit_end - unit)));
         kvh = group / f.pair_groups;
         pg = group - kvh * f.pair_groups;
-        r0 = max(a.row_start[r], 0);
+        r0 = rows_of(a.row_start, r, a.n_rows).first;
         len = battn_same(battn_len(a, r));
         last = len - 1;
         pairs = min(PAIRS, f.n * a.group - pg * PAIRS);       // (rows times heads: at most those of a call)

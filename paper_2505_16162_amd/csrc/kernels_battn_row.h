@@ -17,8 +17,9 @@ __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = blockIdx.x / a.H, h = blockIdx.x % a.H, kvh = h / a.group;
     if (t >= a.n_rows || t >= a.row_start[a.n_requests]) return;      // the whole workgroup
-    const int r = battn_request(a.row_start, a.n_requests, t), r0 = max(a.row_start[r], 0);
-    const int n = a.row_start[r + 1] - r0;
+    const int r = battn_request(a.row_start, a.n_requests, t);
+    const RowsRange rows = rows_of(a.row_start, r, a.n_rows);
+    const int r0 = rows.first, n = rows.n;
     const int len = PAGED ? battn_len(a, r) : n;
     const int last = PAGED ? min(len - n + (t - r0), len - 1) : t - r0;      // the row's own position
     const int d = (lane % LP) * 8, sub = lane / LP + wave * NP;

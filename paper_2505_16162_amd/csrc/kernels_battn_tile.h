@@ -31,10 +31,7 @@ __device__ __forceinline__ bool battn_find_tile(const BattnArgs &a, int index, i
     for (int r0 = 0; r0 < a.n_requests; r0 += 64) {
         const int r = r0 + lane;
         int mine = 0;
-        if (r < a.n_requests) {
-            const long long n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
-            if (n > 0) mine = (int)((n * a.group + BT_PAIRS - 1) / BT_PAIRS);
-        }
+        if (r < a.n_requests) mine = (int)(((long long)rows_of(a.row_start, r, a.n_rows).n * a.group + BT_PAIRS - 1) / BT_PAIRS);
         int upto = mine;
         for (int off = 1; off < 64; off <<= 1) {
             const int u = __shfl_up(upto, off);
@@ -70,7 +67,7 @@ struct TileShape {
 constexpr int BT_FAR = 1 << 24;         // positions beyond count as so many
 __device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r, int positions) {
     TileShape f{0, 0, 0, 0, 0, (long long)positions * a.group};
-    const int n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
+    const int n = rows_of(a.row_start, r, a.n_rows).n;
     if (n > 0) {
         f.n = n;
         f.pairs = (long long)n * a.group;
@@ -153,7 +150,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
         kvh = blockIdx.x % a.Hkv;                             // (a kv head's tiles run behind few L2s)
         if (!battn_find_tile(a, blockIdx.x / a.Hkv, r, tile, f.tiles)) return;
         tile = f.tiles - 1 - tile;                            // long ones first
-        f.n = min(a.row_start[r + 1], a.n_rows) - max(a.row_start[r], 0);
+        f.n = rows_of(a.row_start, r, a.n_rows).n;
         f.pairs = (long long)f.n * a.group;
     }
     int buf = 0;                                              // where the next block goes
@@ -204,7 +201,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
         v_at[dt] = l0 + KV + v_row * RB + (((32 * dt + v_col) * ELT / 16) ^ value_order(v_row)) * 16 + v_col * ELT % 16;
     }
     auto enter = [&]() __attribute__((always_inline)) {       // the segment of `tile` that begins at `at`
-        r0 = max(a.row_start[r], 0);
+        r0 = rows_of(a.row_start, r, a.n_rows).first;
         n = battn_same(f.n);
         len = PAGED ? battn_same(battn_len(a, r)) : n;
         last = len - 1;
