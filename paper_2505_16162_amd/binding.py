@@ -223,6 +223,20 @@ def _heads(t: torch.Tensor, device: torch.device, head_dim: int, name: str):
     return t.data_ptr(), (stride[0] if rows > 1 else heads * dim), heads
 
 
+def _output(like: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """A contiguous tensor for a result of like's shape and type, from the memory of the stream that will write it: what the current stream's pool gives may be a
+    block that kernels of that stream, freed by the host already, are still at work on. A result on `stream` is not given away again
+    before what the current stream has done with it by the time it is freed is done."""
+    if stream is None:
+        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        out = torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    current = torch.cuda.current_stream(like.device)
+    if current != stream:
+        out.record_stream(current)
+    return out
+
+
 def _call(device: torch.device, stream: Optional[torch.cuda.Stream], tensors, fn, *args) -> None:
     """fn(*args, stream) on the device's current stream or on `stream`, with that device current. The tensors stay with the
     allocator until what `stream` does with them is done."""
@@ -327,7 +341,8 @@ def knnssd_paged_store(pages: Pages, qkv: torch.Tensor, slots: torch.Tensor, pos
 
 
 def paged_attention_workspace(pages: Pages, n_heads: int, dtype: torch.dtype) -> torch.Tensor:
-    """A workspace for knnssd_paged_attention on these pages with n_heads query heads of `dtype`."""
+    """A workspace for knnssd_paged_attention on these pages with n_heads query heads of `dtype`: memory of the current stream, which another
+    one that a call uses it on has to wait for once."""
     code = _TORCH_CODE.get(dtype)
     size = load_library().knnssd_paged_attention_bytes(pages.ref, int(n_heads), -1 if code is None else code)
     if size == 0:
@@ -339,11 +354,11 @@ def knnssd_paged_attention(pages: Pages, block_table: torch.Tensor, row_start: t
                            out: Optional[torch.Tensor] = None, scale: Optional[float] = None, most_rows: int = 0,
                            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Attention of the batch's new rows, q [rows][n_heads][head_dim], over the pages. scale None: 1 / sqrt(head_dim). Without `out` rows
-    behind the last request's hold whatever was there."""
+    behind the last request's hold whatever was there, and the result is a tensor of `stream` (wait for that before another one reads it)."""
     dev, dim = pages.device, pages.head_dim
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
     qp, qs, n_heads = _heads(q, dev, dim, "q")
+    if out is None:
+        out = _output(q, stream)
     op, os_, _ = _heads(out, dev, dim, "out")
     if out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must have the shape and type of q")
@@ -362,14 +377,14 @@ def knnssd_paged_attention(pages: Pages, block_table: torch.Tensor, row_start: t
 def knnssd_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, out: Optional[torch.Tensor] = None,
                             scale: Optional[float] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Causal attention of packed prompts, each over itself: q [rows][n_heads][head_dim], k and v [rows][n_kv_heads][head_dim] (parts of one row too),
-    row_start int32 [n_requests + 1]. Without `out` rows behind the last prompt's hold whatever was there."""
+    row_start int32 [n_requests + 1]. Without `out` rows behind the last prompt's hold whatever was there, and the result is a tensor of `stream`."""
     dev = q.device
     if dev.type != "cuda" or q.dim() != 3:
         raise ValueError("q must be [rows][n_heads][head_dim] on a GPU")
     dim = q.shape[2]
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
     qp, qs, n_heads = _heads(q, dev, dim, "q")
+    if out is None:
+        out = _output(q, stream)
     kp, ks, n_kv = _heads(k, dev, dim, "k")
     vp, vs, n_v = _heads(v, dev, dim, "v")
     op, os_, _ = _heads(out, dev, dim, "out")
