@@ -372,7 +372,8 @@ int32_t knnssd_paged_store(const knnssd_pages *pages, const void *qkv_dev, int32
  * [n_rows] rows of n_heads * head_dim values in dtype, q_stride / out_stride elements apart; they must not overlap. dtype is
  * the cache's type, or KNNSSD_FP32 over a bf16 cache. Scores, softmax and sums are fp32; with dtype KNNSSD_BF16 the weights are rounded to
  * bf16 for the product with the values. Positions from kv_len on are not looked at; keys and values that a row does not see but a
- * later one of its request does have to be finite. block_table_dev: [n_requests][table_width]. most_rows: an upper bound of a request's rows
+ * later one of its request does have to be finite. Sums are of values times weights that may be more than 1: |value| times the positions of its request has to
+ * stay below 2^96. block_table_dev: [n_requests][table_width]. most_rows: an upper bound of a request's rows
  * if the caller has one, else 0; it only chooses the kernels. How the sums over a row are grouped follows the batch; the same call gives the
  * same bits. ws_dev: knnssd_paged_attention_bytes of the same pages, n_heads and dtype (0: not a supported shape), 256-byte aligned, of any
  * contents; nothing in it outlives a call.

@@ -20,6 +20,10 @@ namespace ks {
 // themselves: a sixteenth of the bf16 rate.
 // ------------------------------------------------------------------------------------------
 constexpr int BT_PAIRS = 128;
+// What a lane's weights of a block may add up to before their reference follows the scores. Sums of values times weights have that much less room: 2^33 times the blocks of an
+// axis, times the values, has to stay below 2^128. Following costs nothing where scores have a standard deviation of 1 or 4; of 8, prompts of 4096 rows take 366 us, as
+// with 2^64, with 2^24 374, with 2^16 391 (chunks 475, 489, 532).
+constexpr float BT_RISE = 0x1p32f;
 // positions of a block: 64, or 32 over prompts in heads of 128, where the registers of a block's scores then leave room for a third wavefront on each SIMD
 // (two prompts of 4096 rows 418 -> 400 us; over pages, whose wavefronts need more of them, 512 -> 522 us)
 template <int HD, bool PAGED, int NP> constexpr int battn_tile_positions() { return NP == 0 ? 32 * 128 / HD : HD == 128 && !PAGED ? 32 : 64; }
@@ -329,16 +333,16 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
                 }
             return ps;
         };
-        // The weights are taken against the largest score of the tile's first block: what comes later may be far above that (weights of up to
-        // 2^64 lose nothing, bf16 and fp32 have the same steps there) before the reference has to follow. So a block's
-        // weights wait for no maximum; a block whose sum shows that it should have been looked for is begun anew.
+        // The weights are taken against the largest score of the tile's first block: what comes later may be above that, its weights more than 1 (bf16 and
+        // fp32 have the same steps there), before the reference has to follow. So a block's weights wait for no maximum; a block whose sum shows that it should
+        // have been looked for is begun anew.
         auto work = [&](int c, auto first_) __attribute__((always_inline)) {
             constexpr bool FIRST = decltype(first_)::value;
             f32x16_t s[CH / 32];
             scores(c, s);
             if constexpr (FIRST) follow(s);
             float ps = weigh(s);
-            if (!FIRST && __builtin_expect(__any(ps > 0x1p64f), 0)) {
+            if (!FIRST && __builtin_expect(__any(ps > BT_RISE), 0)) {
                 scores(c, s);
                 follow(s);
                 ps = weigh(s);
