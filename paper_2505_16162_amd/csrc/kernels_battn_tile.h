@@ -335,14 +335,14 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
         };
         // The weights are taken against the largest score of the tile's first block: what comes later may be above that, its weights more than 1 (bf16 and
         // fp32 have the same steps there), before the reference has to follow. So a block's weights wait for no maximum; a block whose sum shows that it should
-        // have been looked for is begun anew.
+        // have been looked for is begun anew, and so is one behind blocks whose scores were all -inf, however low its own are.
         auto work = [&](int c, auto first_) __attribute__((always_inline)) {
             constexpr bool FIRST = decltype(first_)::value;
             f32x16_t s[CH / 32];
             scores(c, s);
             if constexpr (FIRST) follow(s);
             float ps = weigh(s);
-            if (!FIRST && __builtin_expect(__any(ps > BT_RISE), 0)) {
+            if (!FIRST && __builtin_expect(__any(ps > BT_RISE || ref == -INFINITY), 0)) {
                 scores(c, s);
                 follow(s);
                 ps = weigh(s);

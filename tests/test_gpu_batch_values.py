@@ -62,3 +62,14 @@ def test_large_values_under_scores_that_rise(rows, lens, types):
     """Scores 0 in the first block and 38 (55 powers of two) behind it, values around 1e24: the outputs are as large as the values, and finite."""
     g = torch.Generator().manual_seed(1)
     check(*batch(rows, lens, types, lambda p: 38.0 * (p >= FIRST), 1e24, g), types)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("rows,lens", BATCHES)
+def test_first_positions_whose_scores_fp32_does_not_hold(rows, lens, types):
+    """Keys of -3e38 give the first block's positions scores of -inf: they have no weight, however far below zero the scores behind them are."""
+    g = torch.Generator().manual_seed(2)
+    q, k, v = batch(rows, lens, types, lambda p: -140.0 - (p % 5), 1.0, g)
+    for t in k:
+        t[:FIRST] = -3e38
+    check(q, k, v, types, hidden=FIRST)
