@@ -357,7 +357,7 @@ int32_t knnssd_page_plan(const knnssd_page_tables *tables, const int32_t *cached
 
 /* Rotary embedding of a block's queries and keys, and its keys and values into the pages. qkv_dev: [n_rows] rows, qkv_stride elements
  * apart, of n_heads query heads, then the keys of the kv heads, then their values, head_dim values each (the rows of wqkv), in dtype. Pairs
- * (i, i + head_dim/2) are turned by position * rope_base^(-2i/head_dim): angles in 64 bits, products in fp32, one
+ * (i, i + head_dim/2) are turned by position * rope_base^(-2i/head_dim): angles in 64 bits up to whole turns, the rest's sine and cosine and the products in fp32, one
  * rounding to what is stored. Rotated queries go to q_out_dev (NULL: nowhere), rotated keys also to k_out_dev (NULL: only into the pages),
  * both in dtype, rows q_out_stride / k_out_stride elements apart; either may lie over the same heads of qkv_dev. Keys and values go to
  * page slot / page_size, position slot % page_size, in the cache's type. A row whose slot is negative or outside the cache, or whose position is
@@ -372,9 +372,9 @@ int32_t knnssd_paged_store(const knnssd_pages *pages, const void *qkv_dev, int32
  * [n_rows] rows of n_heads * head_dim values in dtype, q_stride / out_stride elements apart; they must not overlap. dtype is
  * the cache's type, or KNNSSD_FP32 over a bf16 cache. Scores, softmax and sums are fp32; with dtype KNNSSD_BF16 the weights are rounded to
  * bf16 for the product with the values. Positions from kv_len on are not looked at; keys and values that a row does not see but a
- * later one of its request does have to be finite. Sums are of values times weights that may be more than 1: |value| times the positions of its request has to
- * stay below 2^96. block_table_dev: [n_requests][table_width]. most_rows: an upper bound of a request's rows
- * if the caller has one, else 0; it only chooses the kernels. How the sums over a row are grouped follows the batch; the same call gives the
+ * later one of its request does have to be finite, and a row that sees an infinite value may have NaN where its output would be
+ * infinite. Sums are of values times weights that may be more than 1: |value| times the positions of its request has to stay below
+ * 2^96. block_table_dev: [n_requests][table_width]. most_rows: an upper bound of a request's rows if the caller has one, else 0; it only chooses the kernels. How the sums over a row are grouped follows the batch; the same call gives the
  * same bits. ws_dev: knnssd_paged_attention_bytes of the same pages, n_heads and dtype (0: not a supported shape), 256-byte aligned, of any
  * contents; nothing in it outlives a call.
  * KNNSSD_ESHAPE where n_heads is not a multiple of n_kv_heads, KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows < 1,

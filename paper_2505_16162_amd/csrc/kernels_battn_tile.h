@@ -15,8 +15,8 @@ namespace ks {
 // exchanged between lanes but one maximum per block.
 // Keys and values come in blocks of 32 or 64 positions straight to LDS, one block ahead.
 // What bounds it: over prompts and chunks the vector unit (exponentials, packing) beside the matrix cores, which do not wait for one another within a wavefront but do
-// between two products of one; two or three wavefronts on a SIMD fill that partly. Two prompts of 4096 rows, 40 heads of 128, bf16: 366 us = 938 TFLOP/s (matrix cores busy
-// 51 % of the time, the vector unit as much; on zeros, where the power limit leaves more clock, a quarter faster); eight chunks of up to 900 rows over 700 to 9000 positions in pages, 40 heads over 8: 492 us = 770 TFLOP/s. In fp32 the matrix instructions
+// between two products of one; further wavefronts on a SIMD fill that partly (two in all over pages, three over prompts in heads of 128, four in heads of 64). Two prompts of 4096 rows, 40 heads of 128, bf16: 365 us = 941 TFLOP/s (matrix cores busy
+// 51 % of the time, the vector unit as much; on zeros, where the power limit leaves more clock, a quarter faster); eight chunks of up to 900 rows over 700 to 9000 positions in pages, 40 heads over 8: 485 us = 783 TFLOP/s. In fp32 the matrix instructions
 // themselves: a sixteenth of the bf16 rate.
 // ------------------------------------------------------------------------------------------
 constexpr int BT_PAIRS = 128;
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
     } else {
         kvh = blockIdx.x % a.Hkv;                             // (a kv head's tiles run behind few L2s)
         if (!battn_find_tile(a, blockIdx.x / a.Hkv, r, tile, f.tiles)) return;
-        tile = f.tiles - 1 - tile;                            // long ones first
+        tile = f.tiles - 1 - tile;                            // a request's long ones first (the requests in their own order)
         f.n = rows_of(a.row_start, r, a.n_rows).n;
         f.pairs = (long long)f.n * a.group;
     }

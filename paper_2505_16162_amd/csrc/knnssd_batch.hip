@@ -106,9 +106,12 @@ static void launch_prompt_tiles(const BattnArgs &a, hipStream_t s) {
     hipLaunchKernelGGL((battn_tile_kernel<HD, false, NP>), dim3((unsigned)tiles_bound(a)), dim3(256), (battn_tile_lds<HD, false, NP>()), s, a);
 }
 
-// Most (row, head) pairs of one kv head that a request may have for battn_few_kernel to take the batch: as many as one group holds. 40 heads over 8: 32 requests of
-// one to three rows at 200 to 4000 positions take 61 us, in tiles 66, a single row 9.5 and 14; 20 to 30 pairs, two groups that each read the cache (two requests at 100 000 positions),
-// 159 and 145; 33 to 60 pairs 84 to 195 and 76 to 148.
+// Most (row, head) pairs of one kv head that a request may have for battn_few_kernel to take the batch: as many as one group holds; each further group reads the cache
+// again. Whole calls, us, few rows / tiles, 32 requests at 200 to 4000 positions, bf16 queries; fp32 ones (whose tiles do three times the products):
+//   40 heads of 128 over 8: 5 pairs 62 / 68; 59 / 83, 10 to 15 64 / 72; 67 / 91, 20 77 / 57; 104 / 88, 20 to 30 92 / 63; 85 / 78, 35 to 60 133 / 64; 189 / 118
+//   40 over 40: 1 pair 233 / 271; 240 / 296, 16 293 / 306; 286 / 339, 20 527 / 319; 557 / 404, 60 972 / 384; 1011 / 433
+//   32 heads of 64 over 8: 8 to 12 29 / 31; 34 / 52, 16 34 / 39; 40 / 54, 16 to 24 42 / 38; 51 / 57, 28 to 48 58 / 37; 70 / 64
+// Two requests of 20 to 30 pairs at 100 000 positions 223 / 157; 227 / 167. The bound is the caller's most_rows, or all rows of the batch.
 static const int FEW_PAIRS = 16;
 
 template <int HD, int NP>
@@ -121,8 +124,10 @@ static void launch_few(const BattnArgs &a, int64_t most, hipStream_t s) {
     launch_merge<HD, NP>(a, runs, (int)(most < FEW_PAIRS ? most : FEW_PAIRS), groups * a.Hkv, FEW_PAIRS, s);
 }
 
-// In fp32 the tiles' matrix instructions take 8000 cycles a block, however few pairs a tile has; few rows over short contexts are done sooner by battn_row_kernel
-// (three prompts of up to 45 rows, 4 heads: 5 us, in tiles 8.5; one row of 40 heads over 400 positions 17 and 23, over 1500 positions 52 and 24).
+// In fp32 the tiles' matrix instructions take 8000 cycles a block, however few pairs a tile has; few rows over short contexts are done sooner by battn_row_kernel.
+// What the host knows of a context's length is the most that its table holds, so the same requests go to the tiles under a table for more. Whole calls, us, row kernel / tiles:
+// three prompts of 45 rows, 4 heads of 64, 8 / 15; one row of 40 heads of 128 over 400 positions 11 / 22, eight requests of one 26 / 29; 32 requests of one row,
+// 4 heads of 64, 8 / 27. It loses where many heads of one kv head read the same keys: 32 requests of one row, 40 heads over 8, 400 positions 101 / 44 (100 positions 28 / 28).
 static bool rows_alone(const BattnArgs &a, int64_t positions) { return (int64_t)a.n_rows * a.H < BR_FULL && positions <= 512; }
 
 template <int HD>
