@@ -388,7 +388,7 @@ def _verify(s):
         tried = live[:, j] & (parents[:, j] == node)
         px, qx = p[here, tokens[:, j]], q[here, tokens[:, j]]
         good = tried & (px > ((taken + u[:, j] * left) * qx if drawn else u[:, j] * left))
-        bad = tried & ~good
+        bad = tried & ~good & (qx > 0 if drawn else True)       # (a token that the draft cannot have drawn says nothing about its distribution)
         if drawn:
             taken = torch.where(bad, taken + left, taken)
             left = torch.where(bad, (p - taken[:, None] * q).clamp(min=0).sum(-1), left)
@@ -541,6 +541,8 @@ def _exact_verify(s):
                 if u[a + i] * drawn_from[x] < p[x]:
                     went = i
                     break
+                if drawn_from[x] == 0:                          # the draft cannot have drawn it
+                    continue
                 rest = (p - drawn_from).clamp(min=0) if q is not None else torch.where(drawn_from > 0, 0.0, p)
                 p = rest / rest.sum()
             if went is None:
