@@ -398,6 +398,58 @@ int32_t knnssd_prompt_attention(const void *q_dev, int64_t q_stride, const void 
  * is not a multiple of page_size or page_size is not one that knnssd_pages allows. */
 int32_t knnssd_context_pages(const knnssd_ctx *ctx, int32_t block, int32_t page_size, knnssd_pages *pages_out);
 
+/* ---- Trees of drafted tokens ------------------------------------------------------------------------------------
+ * A batch's new rows may be trees of drafted tokens instead of chains: parents[t] says for row t of the batch which row of its request (0: the request's first) it continues; -1, or
+ * anything that is not an earlier row, makes it a root. Row 0 is the last token that is certain, the others are drafts. A round: knnssd_page_plan, knnssd_tree_plan, for every block
+ * knnssd_paged_store (with the tree's positions) and knnssd_tree_attention, then knnssd_tree_verify and knnssd_tree_keep, whose lengths are the next plan's `cached`.
+ * What is said above of batches holds here too: everything in stream order, capturable, lengths and trees read on the device and bounded there.           */
+#define KNNSSD_MAX_TREE 1024                /* rows of a request's tree */
+#define KNNSSD_MAX_VOCAB (1 << 19)
+
+/* Positions and masks of ancestors. positions_dev [n_rows]: kv_len[r] minus the request's rows plus the row's depth (a root's is 0), over those that knnssd_page_plan wrote (a row's slot stays: the
+ * tree's rows lie in the cache in their own order). masks_dev [n_rows][mask_words], 8-byte aligned: bit j % 64 of word j / 64 says that the row sees row j of its request: itself and its ancestors. A
+ * request has up to 64 * mask_words rows; the masks of further ones are 0 and their positions -1. Rows behind the last request's are left as they were. row_start_dev and kv_len_dev as
+ * knnssd_page_plan wrote them. KNNSSD_ERANGE for mask_words outside [1, KNNSSD_MAX_TREE / 64], n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows outside [1, KNNSSD_MAX_ROW_HEADS / 4]. */
+int32_t knnssd_tree_plan(const int32_t *parents_dev, const int32_t *row_start_dev, const int32_t *kv_len_dev, int32_t n_requests, int32_t n_rows,
+                         int32_t *positions_dev, uint64_t *masks_dev, int32_t mask_words, void *hip_stream);
+
+/* knnssd_paged_attention for rows that see, of their request's new rows, only those up to themselves whose bits in their masks are set (any mask will do: row i sees row j <= i if bit j is set, rows
+ * from 64 * mask_words on have no bit), and all cached positions. A row that sees nothing has an output of 0. Workspace and limits as there; keys and values of
+ * all of a request's new rows have to be finite. masks_dev: [n_rows][mask_words], 8-byte aligned. */
+int32_t knnssd_tree_attention(const knnssd_pages *pages, const int32_t *block_table_dev, int32_t table_width, const int32_t *row_start_dev,
+                              const int32_t *kv_len_dev, int32_t n_requests, const uint64_t *masks_dev, int32_t mask_words, const void *q_dev, int64_t q_stride,
+                              void *out_dev, int64_t out_stride, int32_t dtype, int32_t n_rows, int32_t n_heads, float scale, int32_t most_rows,
+                              void *ws_dev, size_t ws_bytes, void *hip_stream);
+
+/* Drafted tokens tried against the model's probabilities, so that what comes out is distributed as the model's own tokens are. logits_dev: [n_rows] rows of vocab values in dtype, logits_stride
+ * elements apart (any alignment of the type's own), -inf for tokens that are ruled out; row t's are those of the token behind row t. p = softmax(logits / temperature[r]); at a temperature of 0
+ * all of it is on the (first) largest value. From row 0 on the children of the node reached so far are tried in the order of their rows, with the row's number u from u_accept_dev [n_rows]:
+ *   draft_logits_dev given (rows as logits'; a row's are those that its children were drawn from, each for itself, with the same temperature; rows without children are not looked at):
+ *     q = softmax(draft_logits / temperature); c = 0, S = 1 at first; child x is taken if p(x) > (c + u S) q(x), else, if q(x) > 0, c grows by S and S becomes the sum of max(p - c q, 0)
+ *   draft_logits_dev NULL, the drafts were not drawn: child x is taken if p(x) > u S, else S loses p(x) and p(x) becomes 0
+ * Where no child is taken the walk ends, and the next token is the first that the sum of max(p - c q, 0) (or of what is left of p) up to and with it is more than u_next[r] times the whole sum. So a
+ * request of a single row draws a token from its logits. A request's path_dev[row_start[r] + j], j < n_path[r], are its rows taken, row 0 first, -1 behind; next_token_dev[r] comes
+ * behind them. All sums are in 64 bits. Numbers from [0, 1) belong in u_accept_dev and u_next_dev.
+ * next_token[r] is -1 where there is no distribution to go by: a request without rows or with a temperature that is negative or not finite (n_path is 0 then), a row on the path whose logits (or, if it has
+ * children, draft's logits) hold NaN or +inf or nothing but -inf, or nothing left of p. A drafted token outside the vocabulary is never taken; rows from
+ * KNNSSD_MAX_TREE on of a request are none of the tree. most_children: an upper bound of a row's children if the caller has one, else 0; it only chooses the kernels.
+ * ws_dev: knnssd_tree_verify_bytes (drawn: draft_logits_dev is given; 0: sizes that the call refuses), 256-byte aligned, of any contents; nothing in it outlives a call. The same call gives the same result.
+ * KNNSSD_ESHAPE for vocab outside [1, KNNSSD_MAX_VOCAB], KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows outside [1, KNNSSD_MAX_ROW_HEADS / 4] or
+ * n_rows * ceil(vocab / 2048) > KNNSSD_MAX_ROW_HEADS. Outputs must not overlap inputs. */
+size_t knnssd_tree_verify_bytes(int32_t n_rows, int32_t n_requests, int32_t vocab, int32_t drawn);
+int32_t knnssd_tree_verify(const void *logits_dev, int64_t logits_stride, const void *draft_logits_dev, int64_t draft_stride, int32_t dtype, int32_t vocab,
+                           const int32_t *tokens_dev, const int32_t *parents_dev, const int32_t *row_start_dev, int32_t n_requests, int32_t n_rows,
+                           const float *temperature_dev, const float *u_accept_dev, const float *u_next_dev, int32_t *path_dev, int32_t *n_path_dev,
+                           int32_t *next_token_dev, int32_t most_children, void *ws_dev, size_t ws_bytes, void *hip_stream);
+
+/* The path's keys and values side by side: in every one of n_blocks caches (alike in everything but their addresses: KNNSSD_ESHAPE) the entry of row path[row_start[r] + j] of request r goes to position
+ * kv_len[r] - rows + j, for j < n_path[r]; cached_dev[r] becomes the position behind the last of them, the next knnssd_page_plan's `cached`. A path ascends strictly; it ends before an entry that does
+ * not, that is no row of the request or that lies beyond its table. What a request's positions from cached[r] on hold afterwards is of no use. cached_dev must not overlap kv_len_dev or n_path_dev (KNNSSD_EINVAL).
+ * KNNSSD_ERANGE for n_blocks outside [1, 65535], table_width < 1, n_requests or n_rows as in knnssd_tree_plan. */
+int32_t knnssd_tree_keep(const knnssd_pages *blocks, int32_t n_blocks, const int32_t *block_table_dev, int32_t table_width, const int32_t *row_start_dev,
+                         const int32_t *kv_len_dev, int32_t n_requests, int32_t n_rows, const int32_t *path_dev, const int32_t *n_path_dev,
+                         int32_t *cached_dev, void *hip_stream);
+
 /* Message for an error code; for KNNSSD_EHIP the text of the last HIP error of this thread. */
 const char *knnssd_strerror(int32_t code);
 

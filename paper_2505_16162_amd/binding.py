@@ -28,6 +28,7 @@ EXPORTS = [
     "knnssd_set_pass_mode", "knnssd_pass_counts", "knnssd_strerror", "knnssd_stream_next_domain",
     "knnssd_page_plan", "knnssd_paged_store", "knnssd_paged_attention_bytes", "knnssd_paged_attention", "knnssd_prompt_attention",
     "knnssd_context_pages",
+    "knnssd_tree_plan", "knnssd_tree_attention", "knnssd_tree_verify_bytes", "knnssd_tree_verify", "knnssd_tree_keep",
 ]
 
 
@@ -154,6 +155,16 @@ def load_library() -> ctypes.CDLL:
     lib.knnssd_prompt_attention.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i32, i32, i32, i32, i32, f32, vp]
     lib.knnssd_context_pages.restype = i32
     lib.knnssd_context_pages.argtypes = [vp, i32, i32, vp]
+    lib.knnssd_tree_plan.restype = i32
+    lib.knnssd_tree_plan.argtypes = [vp, vp, vp, i32, i32, vp, vp, i32, vp]
+    lib.knnssd_tree_attention.restype = i32
+    lib.knnssd_tree_attention.argtypes = [vp, vp, i32, vp, vp, i32, vp, i32, vp, i64, vp, i64, i32, i32, i32, f32, i32, vp, ctypes.c_size_t, vp]
+    lib.knnssd_tree_verify_bytes.restype = ctypes.c_size_t
+    lib.knnssd_tree_verify_bytes.argtypes = [i32, i32, i32, i32]
+    lib.knnssd_tree_verify.restype = i32
+    lib.knnssd_tree_verify.argtypes = [vp, i64, vp, i64, i32, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
+    lib.knnssd_tree_keep.restype = i32
+    lib.knnssd_tree_keep.argtypes = [vp, i32, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp]
     lib.knnssd_strerror.restype = ctypes.c_char_p
     lib.knnssd_strerror.argtypes = [i32]
     _lib = lib
@@ -363,6 +374,11 @@ def knnssd_paged_attention(pages: Pages, block_table: torch.Tensor, row_start: t
                            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Attention of the batch's new rows, q [rows][n_heads][head_dim], over the pages. scale None: 1 / sqrt(head_dim). Without `out` rows
     behind the last request's hold whatever was there, and the result is a tensor of `stream` (wait for that before another one reads it)."""
+    return _paged_attention(pages, block_table, row_start, kv_len, None, q, workspace, out, scale, most_rows, stream)
+
+
+def _paged_attention(pages: Pages, block_table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor, masks: Optional[torch.Tensor], q: torch.Tensor,
+                     workspace: torch.Tensor, out: Optional[torch.Tensor], scale: Optional[float], most_rows: int, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
     dev, dim = pages.device, pages.head_dim
     qp, qs, n_heads = _heads(q, dev, dim, "q")
     if out is None:
@@ -375,8 +391,10 @@ def knnssd_paged_attention(pages: Pages, block_table: torch.Tensor, row_start: t
     if workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous on {dev}")
     n, width = block_table.shape
-    _call(dev, stream, (pages.k, pages.v, block_table, row_start, kv_len, q, workspace, out), load_library().knnssd_paged_attention, pages.ref,
-          _ints(block_table, dev, 0, "block_table"), width, _ints(row_start, dev, n + 1, "row_start"), _ints(kv_len, dev, n, "kv_len"), n, qp, qs, op, os_,
+    lib = load_library()
+    fn, tree = (lib.knnssd_paged_attention, ()) if masks is None else (lib.knnssd_tree_attention, _masks(masks, dev, q.shape[0]))
+    _call(dev, stream, (pages.k, pages.v, block_table, row_start, kv_len, masks, q, workspace, out), fn, pages.ref,
+          _ints(block_table, dev, 0, "block_table"), width, _ints(row_start, dev, n + 1, "row_start"), _ints(kv_len, dev, n, "kv_len"), n, *tree, qp, qs, op, os_,
           _dtype_code(q, "q"), q.shape[0], n_heads, dim ** -0.5 if scale is None else float(scale), int(most_rows), workspace.data_ptr(),
           workspace.numel() * workspace.element_size())
     return out
@@ -404,6 +422,109 @@ def knnssd_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, r
     _call(dev, stream, (q, k, v, row_start, out), load_library().knnssd_prompt_attention, qp, qs, kp, ks, vp, vs, op, os_, _dtype_code(q, "q"),
           _ints(row_start, dev, 2, "row_start"), n, q.shape[0], n_heads, n_kv, dim, dim ** -0.5 if scale is None else float(scale))
     return out
+
+
+# ---- trees of drafted tokens ----------------------------------------------------------------------------------------
+def _floats(t: torch.Tensor, device: torch.device, least: int, name: str) -> int:
+    """Address of a contiguous float32 tensor of at least `least` entries on `device`."""
+    if t.dtype != torch.float32 or t.device != device or not t.is_contiguous() or t.numel() < least:
+        raise ValueError(f"{name} must be a contiguous float32 tensor of at least {least} entries on {device}")
+    return t.data_ptr()
+
+
+def _masks(t: torch.Tensor, device: torch.device, n_rows: int):
+    """(address, words of a row) of masks."""
+    if t.dtype != torch.int64 or t.device != device or t.dim() != 2 or not t.is_contiguous() or t.shape[0] < n_rows:
+        raise ValueError(f"masks must be a contiguous int64 tensor [{n_rows}][words] on {device}")
+    return t.data_ptr(), t.shape[1]
+
+
+def _on_a_gpu(t: torch.Tensor, name: str) -> torch.device:
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be on a GPU")
+    return t.device
+
+
+def knnssd_tree_plan(parents: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor, positions: torch.Tensor, masks: torch.Tensor,
+                     stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Positions (int32 [rows]) and masks of ancestors (int64 [rows][words], bit j % 64 of word j / 64 for row j of the request) from the rows' parents (int32 [rows], each an
+    earlier row of its request or -1). row_start and kv_len are those of knnssd_page_plan; `positions` may be the ones that it wrote (BatchRows.positions)."""
+    dev, n, rows = _on_a_gpu(parents, "parents"), kv_len.numel(), parents.numel()
+    mp, words = _masks(masks, dev, rows)
+    _call(dev, stream, (parents, row_start, kv_len, positions, masks), load_library().knnssd_tree_plan, _ints(parents, dev, 1, "parents"),
+          _ints(row_start, dev, n + 1, "row_start"), _ints(kv_len, dev, 1, "kv_len"), n, rows, _ints(positions, dev, rows, "positions"), mp, words)
+
+
+def knnssd_tree_attention(pages: Pages, block_table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor, masks: torch.Tensor, q: torch.Tensor,
+                          workspace: torch.Tensor, out: Optional[torch.Tensor] = None, scale: Optional[float] = None, most_rows: int = 0,
+                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """knnssd_paged_attention for rows that see, of their request's new rows, those that their masks (knnssd_tree_plan) have."""
+    return _paged_attention(pages, block_table, row_start, kv_len, masks, q, workspace, out, scale, most_rows, stream)
+
+
+def tree_verify_workspace(n_rows: int, n_requests: int, vocab: int, drawn: bool, device="cuda") -> torch.Tensor:
+    """A workspace for knnssd_tree_verify of up to n_rows rows; drawn: for calls with draft_logits. Memory of the current stream, which another one that a call
+    uses it on has to wait for once."""
+    size = load_library().knnssd_tree_verify_bytes(int(n_rows), int(n_requests), int(vocab), int(bool(drawn)))
+    if size == 0:
+        raise KnnSsdError(-2, "shape not supported")
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def _logits(t: torch.Tensor, device: torch.device, name: str):
+    if t.dim() != 2 or t.device != device or t.stride(1) != 1:
+        raise ValueError(f"{name} must be [rows][vocab] on {device}, a row's values side by side")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def knnssd_tree_verify(logits: torch.Tensor, tokens: torch.Tensor, parents: torch.Tensor, row_start: torch.Tensor, temperature: torch.Tensor, u_accept: torch.Tensor,
+                       u_next: torch.Tensor, workspace: torch.Tensor, draft_logits: Optional[torch.Tensor] = None, path: Optional[torch.Tensor] = None,
+                       n_path: Optional[torch.Tensor] = None, next_token: Optional[torch.Tensor] = None, most_children: int = 0,
+                       stream: Optional[torch.cuda.Stream] = None):
+    """Drafted tokens tried against softmax(logits / temperature): (path, n_path, next_token). logits [rows][vocab], tokens and parents int32 [rows], temperature and u_next
+    float32 [requests], u_accept float32 [rows], the numbers uniform on [0, 1). draft_logits: those that each row's children were drawn from (with the same temperature); None: the drafts were not
+    drawn. path int32 [rows]: a request's rows that were taken, at its first rows' places, -1 behind; n_path, next_token int32 [requests]; made, of `stream`, where they are not given."""
+    dev, n, rows = _on_a_gpu(logits, "logits"), row_start.numel() - 1, tokens.numel()
+    lp, ls = _logits(logits, dev, "logits")
+    dp, ds = (None, 0) if draft_logits is None else _logits(draft_logits, dev, "draft_logits")
+    for t, name in ((logits, "logits"), (draft_logits, "draft_logits")):
+        if t is not None and (t.shape[0] < rows or t.shape[1] != logits.shape[1] or t.dtype != logits.dtype):
+            raise ValueError(f"{name} must be [{rows}][{logits.shape[1]}] of {logits.dtype}")
+    if workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {dev}")
+    path = _output(tokens, stream) if path is None else path
+    n_path, next_token = (_output(row_start[:n], stream) if t is None else t for t in (n_path, next_token))
+    _call(dev, stream, (logits, draft_logits, tokens, parents, row_start, temperature, u_accept, u_next, workspace, path, n_path, next_token),
+          load_library().knnssd_tree_verify, lp, ls, dp, ds, _dtype_code(logits, "logits"), logits.shape[1], _ints(tokens, dev, 1, "tokens"),
+          _ints(parents, dev, rows, "parents"), _ints(row_start, dev, 2, "row_start"), n, rows, _floats(temperature, dev, n, "temperature"),
+          _floats(u_accept, dev, rows, "u_accept"), _floats(u_next, dev, n, "u_next"), _ints(path, dev, rows, "path"), _ints(n_path, dev, n, "n_path"),
+          _ints(next_token, dev, n, "next_token"), int(most_children), workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return path, n_path, next_token
+
+
+class PageBlocks:
+    """The caches of a model's blocks (Pages of one shape, type and order), as knnssd_tree_keep takes them."""
+
+    def __init__(self, blocks: Sequence[Pages]):
+        self.blocks = list(blocks)
+        if not self.blocks or any(p.device != self.blocks[0].device for p in self.blocks):
+            raise ValueError("blocks must be the caches of one GPU")
+        self.device = self.blocks[0].device
+        self.tensors = [t for p in self.blocks for t in (p.k, p.v)]
+        self.structs = (PagesStruct * len(self.blocks))(*[p.struct for p in self.blocks])
+
+
+def knnssd_tree_keep(blocks: PageBlocks, block_table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor, path: torch.Tensor, n_path: torch.Tensor,
+                     cached: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """The keys and values of the rows on each request's path (knnssd_tree_verify) to the positions behind its cached ones, in all blocks; cached (int32 [requests]) becomes
+    the requests' new lengths. It must not be kv_len or n_path."""
+    dev = blocks.device
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [n_requests][table_width]")
+    n, width = block_table.shape
+    _call(dev, stream, (*blocks.tensors, block_table, row_start, kv_len, path, n_path, cached), load_library().knnssd_tree_keep, blocks.structs, len(blocks.blocks),
+          _ints(block_table, dev, 0, "block_table"), width, _ints(row_start, dev, n + 1, "row_start"), _ints(kv_len, dev, n, "kv_len"), n, path.numel(),
+          _ints(path, dev, 1, "path"), _ints(n_path, dev, n, "n_path"), _ints(cached, dev, n, "cached"))
 
 
 class KnnSsd:

@@ -8,7 +8,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libknnssd.so")
-SOURCES = ["knnssd.hip", "knnssd_batch.hip"]     # compiled side by side
+SOURCES = ["knnssd.hip", "knnssd_batch.hip", "knnssd_tree.hip"]     # compiled side by side
 NO_SPILL_KERNELS = ["gemv_kernel", "gemm_mfma_kernel", "prefill_gemm_kernel", "prefill_thin_kernel", "prefill_attn_kernel"]     # mangled-name fragments of the kernels that must not spill
 
 

@@ -7,9 +7,6 @@
 
 namespace ks {
 
-// ints that nothing writes while the kernel runs, by scalar loads where the index is the same for all lanes
-typedef const __attribute__((address_space(4))) int *const_ints;
-
 struct BattnArgs {
     const void *q, *k, *v;
     void *out;
@@ -21,17 +18,30 @@ struct BattnArgs {
     int H, Hkv, group;
     float scale2;                               // scale * log2(e): softmax in powers of two
     void *ws;
+    const unsigned long long *masks;            // trees: which new rows a row sees, mask_words words a row
+    int mask_words;
 };
 
-// request of row t < row_start[n], by bisection
-__device__ __forceinline__ int battn_request(const_ints row_start, int n, int t) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (row_start[mid] <= t) lo = mid;
-        else hi = mid;
+// What a row of a tree sees of the new rows of its request: bit j of its mask for row j. The first word is at hand (it is all that trees of up to 64 rows have).
+struct BattnMask {
+    unsigned long long first;
+    const unsigned long long *words;
+    int n;
+    __device__ __forceinline__ unsigned long long word(int w) const { return w < 0 ? ~0ull : w == 0 ? first : w < n ? words[w] : 0ull; }
+    // bits j .. j+63; rows before the first are cached positions, which all rows see
+    __device__ __forceinline__ unsigned long long from(int j) const {
+        const int w = max(j, -64) >> 6, sh = max(j, -64) & 63;
+        return sh ? word(w) >> sh | word(w + 1) << (64 - sh) : word(w);
     }
-    return lo;
+    // the same up to row `own`, the row itself
+    __device__ __forceinline__ unsigned long long seen(int j, int own) const {
+        const int n_own = own - j + 1;
+        return n_own <= 0 ? 0ull : n_own >= 64 ? from(j) : from(j) & ((1ull << n_own) - 1);
+    }
+};
+__device__ __forceinline__ BattnMask battn_mask(const BattnArgs &a, int row) {
+    const unsigned long long *words = a.masks + (long long)row * a.mask_words;
+    return BattnMask{words[0], words, a.mask_words};
 }
 
 // positions of request r: what its table can hold at most, and no more than 2^30

@@ -7,6 +7,20 @@ namespace ks {
 
 typedef uint16_t bf16_t;  // raw bit pattern
 
+// ints that nothing writes while the kernel runs, by scalar loads where the index is the same for all lanes
+typedef const __attribute__((address_space(4))) int *const_ints;
+
+// request of row t < row_start[n], by bisection
+__device__ __forceinline__ int battn_request(const_ints row_start, int n, int t) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (row_start[mid] <= t) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
 __device__ __forceinline__ float bf16_to_float(bf16_t b) { return __uint_as_float(((uint32_t)b) << 16); }
 
 // fp32 -> bf16, round to nearest even (inf/nan pass through with the payload truncated)

@@ -33,7 +33,8 @@ __device__ __forceinline__ FewShape battn_few_shape(const BattnArgs &a, int r, i
     return f;
 }
 
-template <int HD, int NP>
+// TREE: of the new rows a row sees those that its mask has.
+template <int HD, int NP, bool TREE>
 __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
     constexpr int QS = HD / 32, DT = HD / 16, MROW = HD + BF_PAD, PAIRS = 16, CH = battn_few_positions<HD>(), PT = CH / 16;
     typedef unsigned int vword __attribute__((ext_vector_type(DT / 2)));
@@ -98,6 +99,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
     vword vr[PT][4];                                          // position 16 pt + 4 kg + i, dimensions DT n16 ...
     int page[PT][2];
     u32x4_t qv[QS][NP == 1 ? 1 : 2];                          // the next group's queries: pair n16, dimensions 32 ks + 8 kg ...
+    BattnMask next_mask{};                                    // ... and the mask of its row
     // first position of the block's e-th eight of tile pt (a page holds at least eight); positions past the last one repeat it
     auto eight = [&](int b, int pt, int e) __attribute__((always_inline)) { return min(b * CH + pt * 16 + e * 8, last & -8); };
     auto look_up = [&](int b) __attribute__((always_inline)) {
@@ -163,6 +165,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
         vb = (const bf16_t *)a.v + kvh * a.head_stride;
         any = len > 0 && b0 + wave < b1;
         if (any) look_up(b0 + wave);
+        if constexpr (TREE) next_mask = battn_mask(a, r0 + (pg * PAIRS + min(n16, pairs - 1)) / a.group);
         if constexpr (NP == 1) load_queries();                // (there is no room for fp32 ones beside the last group's)
         if (any) {
             load_keys(b0 + wave);
@@ -174,6 +177,7 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
     while (true) {
         const int base = len - f.n;
         const int limit = base + (pg * PAIRS + min(n16, pairs - 1)) / a.group, first_limit = base + pg * PAIRS / a.group;      // last visible position of the lane's pair, of the first
+        const BattnMask mask = next_mask;
         bf16x8_t qf[QS][NP];
         if constexpr (NP == 3) load_queries();
 #pragma unroll
@@ -208,7 +212,16 @@ __global__ __launch_bounds__(256, 2) void battn_few_kernel(BattnArgs a) {
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (more) load_keys(b + 4);
             __builtin_amdgcn_sched_barrier(0);
-            if (pos0 + CH - 1 > first_limit) {
+            if constexpr (TREE) {
+                if (pos0 + CH > base) {
+                    const unsigned long long seen = mask.seen(pos0 - base, limit - base) >> (4 * kg);
+#pragma unroll
+                    for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (!(seen >> (pt * 16 + i) & 1)) s[pt][i] = -INFINITY;
+                }
+            } else if (pos0 + CH - 1 > first_limit) {
 #pragma unroll
                 for (int pt = 0; pt < PT; ++pt)
 #pragma unroll

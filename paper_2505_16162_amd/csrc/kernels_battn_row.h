@@ -10,7 +10,8 @@ namespace ks {
 // (34 requests of up to 8 rows, 5 heads, 100 to 350 positions: 19 us; with one wavefront and one step at a time 59).
 constexpr int BR_FULL = 4096;                                 // (row, head) items from which the tiles are taken instead
 
-template <int HD, bool PAGED>
+// TREE (pages): of the new rows a row sees those that its mask has.
+template <int HD, bool PAGED, bool TREE>
 __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
     constexpr int LP = HD / 8, NP = 64 / LP, U = 4, W = 4;
     __shared__ float part[4][HD + 2];
@@ -22,6 +23,8 @@ __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
     const int r0 = rows.first, n = rows.n;
     const int len = PAGED ? battn_len(a, r) : n;
     const int last = PAGED ? min(len - n + (t - r0), len - 1) : t - r0;      // the row's own position
+    BattnMask mask{};
+    if constexpr (TREE) mask = battn_mask(a, t);
     const int d = (lane % LP) * 8, sub = lane / LP + wave * NP;
     float q[8], o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const float *qp = (const float *)a.q + t * a.q_stride + h * HD + d;
@@ -54,7 +57,12 @@ __global__ __launch_bounds__(256) void battn_row_kernel(BattnArgs a) {
             for (int e = 0; e < 8; ++e) s[u] = fmaf(q[e], k[u][e], s[u]);
 #pragma unroll
             for (int off = 1; off < LP; off <<= 1) s[u] += lane_xor(s[u], off);
-            s[u] = p0 + u * NP * W <= last ? s[u] * a.scale2 : -INFINITY;
+            bool sees = p0 + u * NP * W <= last;
+            if constexpr (TREE) {
+                const int j = p0 + u * NP * W - (len - n);
+                if (j >= 0) sees = sees && (mask.word(j >> 6) >> (j & 63) & 1);
+            }
+            s[u] = sees ? s[u] * a.scale2 : -INFINITY;
             top = fmaxf(top, s[u]);
         }
         const float ref = top == -INFINITY ? 0.f : top, f = exp2f(m - ref);

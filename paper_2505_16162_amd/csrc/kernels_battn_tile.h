@@ -84,8 +84,10 @@ __device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r,
 
 // NP: 1 all in bf16; 3 fp32 queries over a bf16 cache, which stay exact as three bf16 planes, as do the weights; 0 all in fp32, on the fp32 matrix
 // instructions (two positions, or dimensions, each), which take keys, values and weights as they lie.
-template <int HD, bool PAGED, int NP>
+// TREE (pages): of the new rows a row sees those that its mask has.
+template <int HD, bool PAGED, int NP, bool TREE>
 __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void battn_tile_kernel(BattnArgs a) {
+    static_assert(PAGED || !TREE, "");
     constexpr int KS = HD / 16, DT = HD / 32, ELT = NP == 0 ? 4 : 2, RB = HD * ELT, SL = RB / 16, MROW = HD + BF_PAD;
     constexpr int CH = battn_tile_positions<HD, PAGED, NP>(), KV = CH * RB;                             // bytes of a block's keys (or values)
     constexpr int ROWS = 64 / SL, NI = KV / 1024 / 4;         // rows a wavefront's load covers, loads per wavefront for the keys
@@ -265,6 +267,8 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
                 }
             }
         }
+        BattnMask mask{};
+        if constexpr (TREE) mask = battn_mask(a, r0 + row);
         float ref = -INFINITY, l = 0.f;
         f32x16_t o[DT];
 #pragma unroll
@@ -299,7 +303,16 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
                     }
                 }
             }
-            if (c * CH + CH - 1 > base + wave_first) {  // some of the block's positions lie behind some of the wavefront's rows
+            if constexpr (TREE) {
+                if (c * CH + CH > base) {               // the block has new rows
+                    const unsigned long long seen = mask.seen(c * CH - base, row) >> (4 * half);
+#pragma unroll
+                    for (int t = 0; t < CH / 32; ++t)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (!(seen >> (t * 32 + 8 * (i / 4) + i % 4) & 1)) s[t][i] = -INFINITY;
+                }
+            } else if (c * CH + CH - 1 > base + wave_first) {  // some of the block's positions lie behind some of the wavefront's rows
 #pragma unroll
                 for (int t = 0; t < CH / 32; ++t)
 #pragma unroll

@@ -95,15 +95,15 @@ static void launch_merge(const BattnArgs &a, unsigned runs, int pairs, int64_t g
 // tiles at most; what is too much ends at once
 static int64_t tiles_bound(const BattnArgs &a) { return (((int64_t)a.n_rows * a.group + BT_PAIRS - 1) / BT_PAIRS + a.n_requests) * a.Hkv; }
 
-template <int HD, int NP>
+template <int HD, int NP, bool TREE>
 static void launch_paged_tiles(const BattnArgs &a, int64_t most, hipStream_t s) {
-    hipLaunchKernelGGL((battn_tile_kernel<HD, true, NP>), dim3(BF_WGS), dim3(256), (battn_tile_lds<HD, true, NP>()), s, a);
+    hipLaunchKernelGGL((battn_tile_kernel<HD, true, NP, TREE>), dim3(BF_WGS), dim3(256), (battn_tile_lds<HD, true, NP>()), s, a);
     launch_merge<HD, NP == 1 ? 1 : 3>(a, BF_WGS, (int)(most < BT_PAIRS ? most : BT_PAIRS), tiles_bound(a), BT_PAIRS, s);
 }
 
 template <int HD, int NP>
 static void launch_prompt_tiles(const BattnArgs &a, hipStream_t s) {
-    hipLaunchKernelGGL((battn_tile_kernel<HD, false, NP>), dim3((unsigned)tiles_bound(a)), dim3(256), (battn_tile_lds<HD, false, NP>()), s, a);
+    hipLaunchKernelGGL((battn_tile_kernel<HD, false, NP, false>), dim3((unsigned)tiles_bound(a)), dim3(256), (battn_tile_lds<HD, false, NP>()), s, a);
 }
 
 // Most (row, head) pairs of one kv head that a request may have for battn_few_kernel to take the batch: as many as one group holds; each further group reads the cache
@@ -114,13 +114,13 @@ static void launch_prompt_tiles(const BattnArgs &a, hipStream_t s) {
 // Two requests of 20 to 30 pairs at 100 000 positions 223 / 157; 227 / 167. The bound is the caller's most_rows, or all rows of the batch.
 static const int FEW_PAIRS = 16;
 
-template <int HD, int NP>
+template <int HD, int NP, bool TREE>
 static void launch_few(const BattnArgs &a, int64_t most, hipStream_t s) {
     const int ch = battn_few_positions<HD>();
     const int64_t blocks = (((int64_t)a.width << a.shift) + ch - 1) / ch, groups = ((int64_t)a.n_rows * a.group + FEW_PAIRS - 1) / (FEW_PAIRS) + a.n_requests;
     const int64_t units = blocks < INT32_MAX ? blocks * groups * a.Hkv : INT64_MAX;      // at most
     const unsigned runs = (unsigned)(units / 4 + 1 < BF_WGS ? (units / 4 + 8) & -8 : BF_WGS);
-    hipLaunchKernelGGL((battn_few_kernel<HD, NP>), dim3(runs), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((battn_few_kernel<HD, NP, TREE>), dim3(runs), dim3(256), 0, s, a);
     launch_merge<HD, NP>(a, runs, (int)(most < FEW_PAIRS ? most : FEW_PAIRS), groups * a.Hkv, FEW_PAIRS, s);
 }
 
@@ -130,25 +130,25 @@ static void launch_few(const BattnArgs &a, int64_t most, hipStream_t s) {
 // 4 heads of 64, 8 / 27. It loses where many heads of one kv head read the same keys: 32 requests of one row, 40 heads over 8, 400 positions 101 / 44 (100 positions 28 / 28).
 static bool rows_alone(const BattnArgs &a, int64_t positions) { return (int64_t)a.n_rows * a.H < BR_FULL && positions <= 512; }
 
-template <int HD>
+template <int HD, bool TREE>
 static void launch_paged(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, int32_t most_rows, hipStream_t s) {
     const int64_t most = (int64_t)(most_rows > 0 && most_rows < a.n_rows ? most_rows : a.n_rows) * a.group;
     if (kv_dtype == KNNSSD_FP32) {
-        if (rows_alone(a, (int64_t)a.width << a.shift)) hipLaunchKernelGGL((battn_row_kernel<HD, true>), dim3((unsigned)(a.n_rows * a.H)), dim3(256), 0, s, a);
-        else launch_paged_tiles<HD, 0>(a, most, s);
+        if (rows_alone(a, (int64_t)a.width << a.shift)) hipLaunchKernelGGL((battn_row_kernel<HD, true, TREE>), dim3((unsigned)(a.n_rows * a.H)), dim3(256), 0, s, a);
+        else launch_paged_tiles<HD, 0, TREE>(a, most, s);
     } else if (most <= FEW_PAIRS) {
-        if (dtype == KNNSSD_FP32) launch_few<HD, 3>(a, most, s);
-        else launch_few<HD, 1>(a, most, s);
+        if (dtype == KNNSSD_FP32) launch_few<HD, 3, TREE>(a, most, s);
+        else launch_few<HD, 1, TREE>(a, most, s);
     } else {
-        if (dtype == KNNSSD_FP32) launch_paged_tiles<HD, 3>(a, most, s);
-        else launch_paged_tiles<HD, 1>(a, most, s);
+        if (dtype == KNNSSD_FP32) launch_paged_tiles<HD, 3, TREE>(a, most, s);
+        else launch_paged_tiles<HD, 1, TREE>(a, most, s);
     }
 }
 
 template <int HD>
 static void launch_prompts(const BattnArgs &a, int32_t dtype, hipStream_t s) {
     if (dtype == KNNSSD_BF16) launch_prompt_tiles<HD, 1>(a, s);
-    else if (rows_alone(a, a.n_rows)) hipLaunchKernelGGL((battn_row_kernel<HD, false>), dim3((unsigned)(a.n_rows * a.H)), dim3(256), 0, s, a);
+    else if (rows_alone(a, a.n_rows)) hipLaunchKernelGGL((battn_row_kernel<HD, false, false>), dim3((unsigned)(a.n_rows * a.H)), dim3(256), 0, s, a);
     else launch_prompt_tiles<HD, 0>(a, s);
 }
 
@@ -159,10 +159,11 @@ extern "C" size_t knnssd_paged_attention_bytes(const knnssd_pages *p, int32_t n_
     return battn_few_merges() + 2 * BF_WGS * slot * sizeof(float);
 }
 
-extern "C" int32_t knnssd_paged_attention(const knnssd_pages *p, const int32_t *block_table_dev, int32_t table_width,
-                                          const int32_t *row_start_dev, const int32_t *kv_len_dev, int32_t n_requests, const void *q_dev,
-                                          int64_t q_stride, void *out_dev, int64_t out_stride, int32_t dtype, int32_t n_rows, int32_t n_heads,
-                                          float scale, int32_t most_rows, void *ws_dev, size_t ws_bytes, void *hip_stream) {
+// attention over pages, of rows that see all earlier ones (masks NULL) or those that their masks have
+static int32_t paged_attention(const knnssd_pages *p, const int32_t *block_table_dev, int32_t table_width, const int32_t *row_start_dev, const int32_t *kv_len_dev,
+                               int32_t n_requests, const uint64_t *masks_dev, int32_t mask_words, const void *q_dev, int64_t q_stride, void *out_dev,
+                               int64_t out_stride, int32_t dtype, int32_t n_rows, int32_t n_heads, float scale, int32_t most_rows, void *ws_dev, size_t ws_bytes,
+                               void *hip_stream) {
     KS_TRY(pages_check(p));
     if (!block_table_dev || !kv_len_dev || !ws_dev) return KNNSSD_EINVAL;
     KS_TRY(rows_check(row_start_dev, n_requests, q_dev, q_stride, out_dev, out_stride, dtype, n_rows, n_heads, p->n_kv_heads, p->head_dim, scale));
@@ -177,10 +178,30 @@ extern "C" int32_t knnssd_paged_attention(const knnssd_pages *p, const int32_t *
     a.H = n_heads; a.Hkv = p->n_kv_heads; a.group = n_heads / p->n_kv_heads;
     a.scale2 = scale * 1.4426950408889634f;
     a.ws = ws_dev;
-    if (p->head_dim == 128) launch_paged<128>(a, dtype, p->kv_dtype, most_rows, (hipStream_t)hip_stream);
-    else launch_paged<64>(a, dtype, p->kv_dtype, most_rows, (hipStream_t)hip_stream);
+    a.masks = (const unsigned long long *)masks_dev; a.mask_words = mask_words;
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (masks_dev) p->head_dim == 128 ? launch_paged<128, true>(a, dtype, p->kv_dtype, most_rows, s) : launch_paged<64, true>(a, dtype, p->kv_dtype, most_rows, s);
+    else p->head_dim == 128 ? launch_paged<128, false>(a, dtype, p->kv_dtype, most_rows, s) : launch_paged<64, false>(a, dtype, p->kv_dtype, most_rows, s);
     HIP_TRY(hipGetLastError());
     return KNNSSD_OK;
+}
+
+extern "C" int32_t knnssd_paged_attention(const knnssd_pages *p, const int32_t *block_table_dev, int32_t table_width,
+                                          const int32_t *row_start_dev, const int32_t *kv_len_dev, int32_t n_requests, const void *q_dev,
+                                          int64_t q_stride, void *out_dev, int64_t out_stride, int32_t dtype, int32_t n_rows, int32_t n_heads,
+                                          float scale, int32_t most_rows, void *ws_dev, size_t ws_bytes, void *hip_stream) {
+    return paged_attention(p, block_table_dev, table_width, row_start_dev, kv_len_dev, n_requests, nullptr, 0, q_dev, q_stride, out_dev, out_stride, dtype, n_rows,
+                           n_heads, scale, most_rows, ws_dev, ws_bytes, hip_stream);
+}
+
+extern "C" int32_t knnssd_tree_attention(const knnssd_pages *p, const int32_t *block_table_dev, int32_t table_width, const int32_t *row_start_dev,
+                                         const int32_t *kv_len_dev, int32_t n_requests, const uint64_t *masks_dev, int32_t mask_words, const void *q_dev,
+                                         int64_t q_stride, void *out_dev, int64_t out_stride, int32_t dtype, int32_t n_rows, int32_t n_heads, float scale,
+                                         int32_t most_rows, void *ws_dev, size_t ws_bytes, void *hip_stream) {
+    if (!masks_dev || ((uintptr_t)masks_dev & 7)) return KNNSSD_EINVAL;
+    if (!mask_words_ok(mask_words)) return KNNSSD_ERANGE;
+    return paged_attention(p, block_table_dev, table_width, row_start_dev, kv_len_dev, n_requests, masks_dev, mask_words, q_dev, q_stride, out_dev, out_stride, dtype,
+                           n_rows, n_heads, scale, most_rows, ws_dev, ws_bytes, hip_stream);
 }
 
 extern "C" int32_t knnssd_prompt_attention(const void *q_dev, int64_t q_stride, const void *k_dev, int64_t k_stride, const void *v_dev,

@@ -1,0 +1,125 @@
+// Host side of the calls for trees of drafted tokens: plan, verification, keeping a path. (Attention: knnssd_batch.hip.)
+#include <hip/hip_runtime.h>
+
+#include "hip_try.h"
+#include "kernels_tree.h"
+#include "kernels_tverify.h"
+#include "pages_check.h"
+
+using namespace ks;
+
+static const_ints ints(const int32_t *p) { return (const_ints)(uintptr_t)p; }
+
+// what every call on a batch's rows is given
+static int32_t batch_check(const int32_t *row_start_dev, int32_t n_requests, int32_t n_rows) {
+    if (!row_start_dev) return KNNSSD_EINVAL;
+    return n_requests < 1 || n_requests > KNNSSD_MAX_REQUESTS || n_rows < 1 || n_rows > KNNSSD_MAX_ROW_HEADS / 4 ? KNNSSD_ERANGE : KNNSSD_OK;
+}
+
+extern "C" int32_t knnssd_tree_plan(const int32_t *parents_dev, const int32_t *row_start_dev, const int32_t *kv_len_dev, int32_t n_requests, int32_t n_rows,
+                                    int32_t *positions_dev, uint64_t *masks_dev, int32_t mask_words, void *hip_stream) {
+    if (!parents_dev || !kv_len_dev || !positions_dev || !masks_dev || ((uintptr_t)masks_dev & 7)) return KNNSSD_EINVAL;
+    KS_TRY(batch_check(row_start_dev, n_requests, n_rows));
+    if (!mask_words_ok(mask_words)) return KNNSSD_ERANGE;
+    TreePlanArgs a{};
+    a.parents = parents_dev; a.row_start = ints(row_start_dev); a.kv_len = ints(kv_len_dev); a.masks = (unsigned long long *)masks_dev; a.positions = positions_dev;
+    a.n_rows = n_rows; a.words = mask_words;
+    hipLaunchKernelGGL(tree_plan_kernel, dim3(n_requests), dim3(64 * mask_words), 0, (hipStream_t)hip_stream, a);
+    HIP_TRY(hipGetLastError());
+    return KNNSSD_OK;
+}
+
+static int tv_chunks(int32_t vocab) { return (vocab + TV_CHUNK - 1) / TV_CHUNK; }
+
+// where in the workspace what lies
+struct TvLayout { size_t states, sums, total; };
+static TvLayout tv_layout(int64_t n_rows, int64_t n_requests, int32_t vocab, bool drawn) {
+    TvLayout l{};
+    l.states = (size_t)n_rows * tv_chunks(vocab) * sizeof(TvStat) * (drawn ? 2 : 1);
+    l.sums = l.states + (drawn ? n_requests * sizeof(TvState) : 0);
+    l.total = (l.sums + (drawn ? n_requests * tv_chunks(vocab) * sizeof(double) : 0) + 255) / 256 * 256;
+    return l;
+}
+
+static int32_t tv_sizes_check(int32_t n_rows, int32_t n_requests, int32_t vocab) {
+    if (n_requests < 1 || n_requests > KNNSSD_MAX_REQUESTS || n_rows < 1 || n_rows > KNNSSD_MAX_ROW_HEADS / 4) return KNNSSD_ERANGE;
+    if (vocab < 1 || vocab > KNNSSD_MAX_VOCAB) return KNNSSD_ESHAPE;
+    return (int64_t)n_rows * tv_chunks(vocab) > KNNSSD_MAX_ROW_HEADS ? KNNSSD_ERANGE : KNNSSD_OK;
+}
+
+extern "C" size_t knnssd_tree_verify_bytes(int32_t n_rows, int32_t n_requests, int32_t vocab, int32_t drawn) {
+    return tv_sizes_check(n_rows, n_requests, vocab) == KNNSSD_OK ? tv_layout(n_rows, n_requests, vocab, drawn != 0).total : 0;
+}
+
+static bool values_ok(const void *base, int64_t stride, int32_t vocab, int32_t dtype) {
+    return !((uintptr_t)base & (dtype_bytes(dtype) - 1)) && stride >= vocab && stride <= INT64_MAX / 8;
+}
+
+template <typename T>
+static void launch_verify(const TvArgs &a, int rounds, hipStream_t s) {
+    const unsigned units = (unsigned)a.n_rows * a.chunks * (a.draft ? 2 : 1);
+    hipLaunchKernelGGL((tv_stats_kernel<T>), dim3((units + 3) / 4), dim3(256), 0, s, a);
+    for (int i = 0; i <= rounds; ++i) {
+        if (i > 0) hipLaunchKernelGGL((tv_sum_kernel<T>), dim3((a.chunks + 3) / 4, a.n_requests), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((tv_walk_kernel<T>), dim3(a.n_requests), dim3(TV_NT), 0, s, a, i, i < rounds);
+    }
+}
+
+extern "C" int32_t knnssd_tree_verify(const void *logits_dev, int64_t logits_stride, const void *draft_logits_dev, int64_t draft_stride, int32_t dtype, int32_t vocab,
+                                      const int32_t *tokens_dev, const int32_t *parents_dev, const int32_t *row_start_dev, int32_t n_requests, int32_t n_rows,
+                                      const float *temperature_dev, const float *u_accept_dev, const float *u_next_dev, int32_t *path_dev, int32_t *n_path_dev,
+                                      int32_t *next_token_dev, int32_t most_children, void *ws_dev, size_t ws_bytes, void *hip_stream) {
+    if (!logits_dev || !tokens_dev || !parents_dev || !row_start_dev || !temperature_dev || !u_accept_dev || !u_next_dev) return KNNSSD_EINVAL;
+    if (!path_dev || !n_path_dev || !next_token_dev || !ws_dev || !dtype_ok(dtype)) return KNNSSD_EINVAL;
+    KS_TRY(tv_sizes_check(n_rows, n_requests, vocab));
+    if (most_children < 0) return KNNSSD_ERANGE;
+    if (!values_ok(logits_dev, logits_stride, vocab, dtype) || (draft_logits_dev && !values_ok(draft_logits_dev, draft_stride, vocab, dtype))) return KNNSSD_EINVAL;
+    if (((uintptr_t)ws_dev & 255) || ws_bytes < knnssd_tree_verify_bytes(n_rows, n_requests, vocab, draft_logits_dev != nullptr)) return KNNSSD_EINVAL;
+    const TvLayout l = tv_layout(n_rows, n_requests, vocab, draft_logits_dev != nullptr);
+    TvArgs a{};
+    a.logits = logits_dev; a.draft = draft_logits_dev; a.logits_stride = logits_stride; a.draft_stride = draft_stride;
+    a.tokens = tokens_dev; a.parents = parents_dev; a.row_start = ints(row_start_dev);
+    a.temperature = temperature_dev; a.u_accept = u_accept_dev; a.u_next = u_next_dev;
+    a.path = path_dev; a.n_path = n_path_dev; a.next = next_token_dev;
+    a.stats = (TvStat *)ws_dev; a.states = (TvState *)((char *)ws_dev + l.states); a.sums = (double *)((char *)ws_dev + l.sums);
+    a.n_requests = n_requests; a.n_rows = n_rows; a.vocab = vocab; a.chunks = tv_chunks(vocab);
+    const int rounds = 0;
+    if (dtype == KNNSSD_BF16) launch_verify<bf16_t>(a, rounds, (hipStream_t)hip_stream);
+    else launch_verify<float>(a, rounds, (hipStream_t)hip_stream);
+    HIP_TRY(hipGetLastError());
+    return KNNSSD_OK;
+}
+
+extern "C" int32_t knnssd_tree_keep(const knnssd_pages *blocks, int32_t n_blocks, const int32_t *block_table_dev, int32_t table_width, const int32_t *row_start_dev,
+                                    const int32_t *kv_len_dev, int32_t n_requests, int32_t n_rows, const int32_t *path_dev, const int32_t *n_path_dev,
+                                    int32_t *cached_dev, void *hip_stream) {
+    if (!blocks || !block_table_dev || !kv_len_dev || !path_dev || !n_path_dev || !cached_dev) return KNNSSD_EINVAL;
+    KS_TRY(batch_check(row_start_dev, n_requests, n_rows));
+    if (n_blocks < 1 || n_blocks > 65535 || table_width < 1) return KNNSSD_ERANGE;
+    const knnssd_pages &p = blocks[0];
+    for (int i = 0; i < n_blocks; ++i) {
+        const knnssd_pages &o = blocks[i];
+        KS_TRY(pages_check(&o));
+        if (o.page_stride != p.page_stride || o.head_stride != p.head_stride || o.pos_stride != p.pos_stride || o.n_pages != p.n_pages || o.page_size != p.page_size ||
+            o.n_kv_heads != p.n_kv_heads || o.head_dim != p.head_dim || o.kv_dtype != p.kv_dtype)
+            return KNNSSD_ESHAPE;
+    }
+    // (the workgroups of other blocks read a request's lengths when the first one may have written what is left of them)
+    for (const int32_t *in : {kv_len_dev, n_path_dev})
+        if (cached_dev < in + n_requests && in < cached_dev + n_requests) return KNNSSD_EINVAL;
+    const int64_t elt = dtype_bytes(p.kv_dtype);
+    TreeKeepArgs a{};
+    a.page_stride = p.page_stride * elt; a.head_stride = p.head_stride * elt; a.pos_stride = p.pos_stride * elt;
+    a.table = ints(block_table_dev); a.row_start = ints(row_start_dev); a.kv_len = ints(kv_len_dev); a.path = ints(path_dev); a.n_path = ints(n_path_dev);
+    a.n_rows = n_rows; a.width = table_width; a.shift = __builtin_ctz((unsigned)p.page_size); a.n_pages = p.n_pages;
+    a.head_pieces = (int)(p.head_dim * elt / 16);
+    a.pieces = p.n_kv_heads * a.head_pieces;
+    for (int b0 = 0; b0 < n_blocks; b0 += KEEP_BLOCKS) {
+        const int n = n_blocks - b0 < KEEP_BLOCKS ? n_blocks - b0 : KEEP_BLOCKS;
+        for (int i = 0; i < n; ++i) { a.k[i] = blocks[b0 + i].k_dev; a.v[i] = blocks[b0 + i].v_dev; }
+        a.cached = b0 == 0 ? cached_dev : nullptr;
+        hipLaunchKernelGGL(tree_keep_kernel, dim3(n_requests, n, (2 * a.pieces + KEEP_NT - 1) / KEEP_NT), dim3(KEEP_NT), 0, (hipStream_t)hip_stream, a);
+    }
+    HIP_TRY(hipGetLastError());
+    return KNNSSD_OK;
+}

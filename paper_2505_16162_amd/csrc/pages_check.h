@@ -30,5 +30,8 @@ static inline int32_t pages_check(const knnssd_pages *p) {
     return p->pos_stride > MAX_ROW_STRIDE ? KNNSSD_ESHAPE : KNNSSD_OK;
 }
 
+// words of a row's mask in a tree
+static inline bool mask_words_ok(int32_t words) { return words >= 1 && words <= KNNSSD_MAX_TREE / 64; }
+
 // the types that rows and a cache may have together
 static inline bool types_go_together(int32_t rows, int32_t cache) { return rows == KNNSSD_FP32 || cache == KNNSSD_BF16; }
