@@ -64,6 +64,7 @@ __global__ __launch_bounds__(KNNSSD_MAX_TREE) void tree_plan_kernel(TreePlanArgs
 
 constexpr int KEEP_BLOCKS = 64, KEEP_NT = 256, KEEP_U = 4;    // blocks of a launch, threads, entries under way
 
+typedef unsigned int keep_piece __attribute__((ext_vector_type(4)));
 struct TreeKeepArgs {
     void *k[KEEP_BLOCKS], *v[KEEP_BLOCKS];
     long long page_stride, head_stride, pos_stride;           // in bytes
@@ -110,13 +111,13 @@ __global__ __launch_bounds__(KEEP_NT) void tree_keep_kernel(TreeKeepArgs a) {
             to[u] = tg * a.page_stride + (t & ((1 << a.shift) - 1)) * a.pos_stride;
             moves[u] = mine;
         }
-        uint4 x[KEEP_U];
+        keep_piece x[KEEP_U];
 #pragma unroll
         for (int u = 0; u < KEEP_U; ++u)
-            if (moves[u]) x[u] = *reinterpret_cast<const uint4 *>(at + from[u]);
+            if (moves[u]) x[u] = *reinterpret_cast<const keep_piece *>(at + from[u]);
 #pragma unroll
         for (int u = 0; u < KEEP_U; ++u)
-            if (moves[u]) *reinterpret_cast<uint4 *>(at + to[u]) = x[u];
+            if (moves[u]) *reinterpret_cast<keep_piece *>(at + to[u]) = x[u];
     }
     if (a.cached && blockIdx.y == 0 && piece == 0) a.cached[r] = (int)(max(base, 0ll) + kept);
 }

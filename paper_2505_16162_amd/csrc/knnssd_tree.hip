@@ -32,10 +32,11 @@ extern "C" int32_t knnssd_tree_plan(const int32_t *parents_dev, const int32_t *r
 static int tv_chunks(int32_t vocab) { return (vocab + TV_CHUNK - 1) / TV_CHUNK; }
 
 // where in the workspace what lies
-struct TvLayout { size_t states, sums, total; };
+struct TvLayout { size_t nodes, states, sums, total; };
 static TvLayout tv_layout(int64_t n_rows, int64_t n_requests, int32_t vocab, bool drawn) {
     TvLayout l{};
-    l.states = (size_t)n_rows * tv_chunks(vocab) * sizeof(TvStat) * (drawn ? 2 : 1);
+    l.nodes = (size_t)n_rows * tv_chunks(vocab) * sizeof(TvStat) * (drawn ? 2 : 1);
+    l.states = l.nodes + (drawn ? n_rows * sizeof(TvNode) : 0);
     l.sums = l.states + (drawn ? n_requests * sizeof(TvState) : 0);
     l.total = (l.sums + (drawn ? n_requests * tv_chunks(vocab) * sizeof(double) : 0) + 255) / 256 * 256;
     return l;
@@ -55,12 +56,18 @@ static bool values_ok(const void *base, int64_t stride, int32_t vocab, int32_t d
     return !((uintptr_t)base & (dtype_bytes(dtype) - 1)) && stride >= vocab && stride <= INT64_MAX / 8;
 }
 
+// How many sums over a row are taken by launches of their own, spread over the chip, before a walk's workgroup takes those that are still needed by itself. A round costs 4 us where no walk waits and
+// about 12 where one does, a sum by one workgroup 0.6 us for every 2048 tokens. Whole calls of 12 requests, us, with 0, 1, 2, 3, 4 rounds:
+//   trees of 8 to 40 rows, 4096 tokens 20, 28, 35, 39, 42; 16384 36, 39, 41, 44, 47; 32000 65, 61, 55, 56, 57; 64000 119, 101, 87, 75, 70; 152064 (6 to 20 rows) 211, 156, 96, 78, 82
+//   chains of 1 to 9 rows, 8192 tokens 19, 25, 28, 31, 40; 32000 35, 29, 32, 35, 39; 152064 102, 42, 44, 47, 50
+static int verify_rounds(int chunks, int most_children) { return chunks <= 8 ? 0 : most_children == 1 ? 1 : chunks <= 24 ? 2 : 4; }
+
 template <typename T>
 static void launch_verify(const TvArgs &a, int rounds, hipStream_t s) {
     const unsigned units = (unsigned)a.n_rows * a.chunks * (a.draft ? 2 : 1);
     hipLaunchKernelGGL((tv_stats_kernel<T>), dim3((units + 3) / 4), dim3(256), 0, s, a);
     for (int i = 0; i <= rounds; ++i) {
-        if (i > 0) hipLaunchKernelGGL((tv_sum_kernel<T>), dim3((a.chunks + 3) / 4, a.n_requests), dim3(256), 0, s, a);
+        if (i > 0) hipLaunchKernelGGL((tv_sum_kernel<T>), dim3(a.chunks, a.n_requests), dim3(256), 0, s, a);
         hipLaunchKernelGGL((tv_walk_kernel<T>), dim3(a.n_requests), dim3(TV_NT), 0, s, a, i, i < rounds);
     }
 }
@@ -81,9 +88,9 @@ extern "C" int32_t knnssd_tree_verify(const void *logits_dev, int64_t logits_str
     a.tokens = tokens_dev; a.parents = parents_dev; a.row_start = ints(row_start_dev);
     a.temperature = temperature_dev; a.u_accept = u_accept_dev; a.u_next = u_next_dev;
     a.path = path_dev; a.n_path = n_path_dev; a.next = next_token_dev;
-    a.stats = (TvStat *)ws_dev; a.states = (TvState *)((char *)ws_dev + l.states); a.sums = (double *)((char *)ws_dev + l.sums);
+    a.stats = (TvStat *)ws_dev; a.nodes = (TvNode *)((char *)ws_dev + l.nodes); a.states = (TvState *)((char *)ws_dev + l.states); a.sums = (double *)((char *)ws_dev + l.sums);
     a.n_requests = n_requests; a.n_rows = n_rows; a.vocab = vocab; a.chunks = tv_chunks(vocab);
-    const int rounds = 0;
+    const int rounds = draft_logits_dev ? verify_rounds(a.chunks, most_children) : 0;        // (only then the workspace has room for walks between rounds)
     if (dtype == KNNSSD_BF16) launch_verify<bf16_t>(a, rounds, (hipStream_t)hip_stream);
     else launch_verify<float>(a, rounds, (hipStream_t)hip_stream);
     HIP_TRY(hipGetLastError());
