@@ -385,23 +385,13 @@ __device__ __forceinline__ void tv_weigh(const TvWeigh &s, const float *v, const
     }
 }
 
-// sum of the weights of the lane's piece-th eight tokens of a chunk, without those that were rejected
+// sum of the weights of eight tokens (and the draft's)
 template <typename T, bool DRAFT>
-__device__ __forceinline__ double tv_weights8(const TvWeigh &s, const T *p, const T *q, int chunk, int piece, int lane, int vocab, const int *rejected, int n_rejected) {
-    TvRaw<T> p_raw, q_raw;
+__device__ __forceinline__ double tv_weights8(const TvWeigh &s, const TvRaw<T> &p, const TvRaw<T> &q) {
     float v[8], w[8];
-    tv_load<T, 1>(p, chunk, piece, lane, vocab, &p_raw);
-    if constexpr (DRAFT) tv_load<T, 1>(q, chunk, piece, lane, vocab, &q_raw);
-    tv_values(p_raw, v);
-    if constexpr (DRAFT) tv_values(q_raw, w);
+    tv_values(p, v);
+    if constexpr (DRAFT) tv_values(q, w);
     double sum = 0.0;
-    if constexpr (!DRAFT)
-        for (int x = 0; x < n_rejected; ++x) {
-            const int d = rejected[x] - tv_at(chunk, piece, lane);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (d == e) v[e] = -INFINITY;
-        }
 #pragma unroll
     for (int e = 0; e < 8; e += 4) {
         double y[4];
@@ -409,6 +399,24 @@ __device__ __forceinline__ double tv_weights8(const TvWeigh &s, const T *p, cons
         sum += (y[0] + y[1]) + (y[2] + y[3]);
     }
     return sum;
+}
+
+// of eight tokens from `at` on, those that were rejected are ruled out
+__device__ __forceinline__ void tv_without(const int *rejected, int n, int at, TvRaw<float> &raw) {
+    for (int x = 0; x < n; ++x) {
+        const int d = rejected[x] - at;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (d == e) raw.w[e >> 2][e & 3] = 0xff800000u;
+    }
+}
+__device__ __forceinline__ void tv_without(const int *rejected, int n, int at, TvRaw<bf16_t> &raw) {
+    for (int x = 0; x < n; ++x) {
+        const int d = rejected[x] - at;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (d == e) raw.w[0][e >> 1] = (raw.w[0][e >> 1] & (e & 1 ? 0xffffu : 0xffff0000u)) | (e & 1 ? 0xff800000u : 0xff80u);
+    }
 }
 
 // Rounds: a rejected draw needs the sum over its whole row before the walk can go on. The walk of `round` stops there if a launch of tv_sum_kernel and another round follow
@@ -593,12 +601,22 @@ __global__ __launch_bounds__(TV_NT) void tv_walk_kernel(TvArgs a, int round, int
             return;
         }
         const TvWeigh w{p_row[node].top, q_row[node].top, tv_least(p_row[node].top, t), tv_least(q_row[node].top, t), 1.0 / p_row[node].sum, c / q_row[node].sum, k};
-        // four wavefronts to a chunk
+        // four wavefronts to a chunk, the next one's values on their way
+        const T *p = logits + node * a.logits_stride, *q = draft + node * a.draft_stride;
+        TvRaw<T> p_raw, q_raw, p_next, q_next;
+        auto load = [&](int x, TvRaw<T> &to_p, TvRaw<T> &to_q) __attribute__((always_inline)) {
+            if (x >= a.chunks) return;
+            tv_load<T, 1>(p, x, wave & 3, lane, a.vocab, &to_p);
+            tv_load<T, 1>(q, x, wave & 3, lane, a.vocab, &to_q);
+        };
+        load(wave / 4, p_raw, q_raw);
         for (int x0 = 0, b = 0; x0 < a.chunks; x0 += TV_WAVES / 4, b ^= 1) {
             const int x = x0 + wave / 4;
+            load(x + TV_WAVES / 4, p_next, q_next);
             double sum = 0.0;
-            if (x < a.chunks)
-                sum = tv_sum(tv_weights8<T, true>(w, logits + node * a.logits_stride, draft + node * a.draft_stride, x, wave & 3, lane, a.vocab, nullptr, 0));
+            if (x < a.chunks) sum = tv_lane(tv_upto(tv_weights8<T, true>(w, p_raw, q_raw)), 63);
+            p_raw = p_next;
+            q_raw = q_next;
             if (lane == 0) part[b][wave] = sum;
             __syncthreads();
             if (x < a.chunks && (tid & 255) == 0) chunk_sum[x] = (part[b][wave] + part[b][wave + 1]) + (part[b][wave + 2] + part[b][wave + 3]);
@@ -627,7 +645,12 @@ __global__ __launch_bounds__(TV_NT) void tv_walk_kernel(TvArgs a, int round, int
         for (int i0 = 0, b = 0; i0 < gone; i0 += TV_WAVES / 4, b ^= 1) {      // chunks with rejected tokens anew (some more than once, to the same end)
             const int i = i0 + wave / 4, x = i < gone ? rejected[i] / TV_CHUNK : 0;
             double sum = 0.0;
-            if (i < gone) sum = tv_sum(tv_weights8<T, false>(w, p, p, x, wave & 3, lane, a.vocab, rejected, gone));
+            if (i < gone) {
+                TvRaw<T> raw;
+                tv_load<T, 1>(p, x, wave & 3, lane, a.vocab, &raw);
+                tv_without(rejected, gone, tv_at(x, wave & 3, lane), raw);
+                sum = tv_lane(tv_upto(tv_weights8<T, false>(w, raw, raw)), 63);
+            }
             if (lane == 0) part[b][wave] = sum;
             __syncthreads();
             if (i < gone && (tid & 255) == 0) chunk_sum[x] = (part[b][wave] + part[b][wave + 1]) + (part[b][wave + 2] + part[b][wave + 3]);
@@ -730,7 +753,10 @@ __global__ __launch_bounds__(256) void tv_sum_kernel(TvArgs a) {
     const TvState s = a.states[r];
     if (!s.waits) return;
     const long long row = rows_of(a.row_start, r, a.n_rows).first + s.node;
-    const double sum = tv_sum(tv_weights8<T, true>(s.w, (const T *)a.logits + row * a.logits_stride, (const T *)a.draft + row * a.draft_stride, chunk, wave, lane, a.vocab, nullptr, 0));
+    TvRaw<T> p, q;
+    tv_load<T, 1>((const T *)a.logits + row * a.logits_stride, chunk, wave, lane, a.vocab, &p);
+    tv_load<T, 1>((const T *)a.draft + row * a.draft_stride, chunk, wave, lane, a.vocab, &q);
+    const double sum = tv_lane(tv_upto(tv_weights8<T, true>(s.w, p, q)), 63);
     if (lane == 0) part[wave] = sum;
     __syncthreads();
     if (threadIdx.x == 0) a.sums[(size_t)r * a.chunks + chunk] = (part[0] + part[1]) + (part[2] + part[3]);
