@@ -161,13 +161,40 @@ __device__ __forceinline__ void battn_few_out(const BattnArgs &a, int r0, int kv
 constexpr int BM_NT = 256;
 template <int HD> __host__ __device__ constexpr int battn_merge_teams() { return BM_NT * 4 / HD; }
 template <int HD, int NP>
-__global__ __launch_bounds__(BM_NT) void battn_merge_kernel(BattnArgs a, int slot_pairs) {
+__global__ __launch_bounds__(BM_NT) void battn_merge_kernel(BattnArgs a, int slot_pairs, int runs) {
     constexpr int LP = HD / 4, TEAMS = battn_merge_teams<HD>(), MROW = HD + BF_PAD, U = 4;
     __shared__ f32x4_t part[TEAMS][LP];
     __shared__ float part_top[TEAMS], part_sum[TEAMS];
-    const int run = battn_run();
-    const FewMerge m = ((const FewMerge *)a.ws)[run];
-    if (m.runs == 0) return;                                  // the whole workgroup
+    // With few groups the grid has a place for each of them: the blockIdx.x-th run in which a group begins that goes on behind it. (A place for every run, most of them
+    // with nothing to do, takes 12 us whatever there is to join: one request's tree of 26 rows 13.7 -> 7.2 us. With many groups the search is what costs: 11.5 against 15.7.)
+    constexpr int WAVES = BM_NT / 64, EACH = BF_WGS / BM_NT;
+    __shared__ int counts[EACH * WAVES], found;
+    const FewMerge *merges = (const FewMerge *)a.ws;
+    const int wave = threadIdx.x >> 6;
+    unsigned long long begins[EACH];
+    int run = battn_run();
+    if (gridDim.x < (unsigned)runs) {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int x = e * BM_NT + threadIdx.x;
+            begins[e] = __ballot(x < runs && merges[min(x, runs - 1)].runs != 0);
+            if ((threadIdx.x & 63) == 0) counts[e * WAVES + wave] = __popcll(begins[e]);
+        }
+        if (threadIdx.x == 0) found = -1;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            int before = 0;
+            for (int x = 0; x < e * WAVES + wave; ++x) before += counts[x];
+            const int l = threadIdx.x & 63;
+            if (begins[e] >> l & 1 && before + __popcll(begins[e] & ((1ull << l) - 1)) == (int)blockIdx.x) found = e * BM_NT + threadIdx.x;
+        }
+        __syncthreads();
+        run = found;
+        if (run < 0) return;                                      // the whole workgroup
+    }
+    const FewMerge m = merges[run];
+    if (m.runs == 0) return;
     const int lane = threadIdx.x % LP, team = threadIdx.x / LP;
     const int subs = m.runs > 8 ? 4 : 1, sub = team & (subs - 1), at_once = TEAMS / subs;
     const size_t slot = battn_few_slot<HD>(slot_pairs);

@@ -62,20 +62,22 @@ template <int HD, bool PAGED, int NP> constexpr int battn_tile_lds() { return 2 
 // x / (a block's cost) of it, and a run of a block's cost or more is never empty. The costs before a tile have a closed form.
 struct TileShape {
     int n, tiles, small;                // rows, tiles of a kv head, those of its first that cost a block
+    bool whole;                         // one cost for all of a kv head's tiles (`tiles` is 1): they are worked on side by side
     long long step, pairs, block;       // cost of a tile without its own pairs; all pairs; a block's cost
     __device__ __forceinline__ long long sloped(int t) const { return t * step + (long long)(BT_PAIRS / 2) * t * (t + 1); }
     __device__ __forceinline__ long long before(int t) const { return t <= small ? t * block : small * block + sloped(t) - sloped(small); }      // (t < tiles)
-    __device__ __forceinline__ long long cost(int t) const { return max(block, step + min((long long)(t + 1) * BT_PAIRS, pairs)); }
+    __device__ __forceinline__ long long cost(int t) const { return max(block, step + (whole ? pairs : min((long long)(t + 1) * BT_PAIRS, pairs))); }
     __device__ __forceinline__ long long total() const { return tiles ? before(tiles - 1) + cost(tiles - 1) : 0; }
 };
 constexpr int BT_FAR = 1 << 24;         // positions beyond count as so many
-__device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r, int positions) {
-    TileShape f{0, 0, 0, 0, 0, (long long)positions * a.group};
+__device__ __forceinline__ int battn_tiles(long long pairs) { return (int)((pairs + BT_PAIRS - 1) / BT_PAIRS); }
+__device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r, int positions, bool whole) {
+    TileShape f{0, 0, 0, whole, 0, 0, (long long)positions * a.group};
     const int n = rows_of(a.row_start, r, a.n_rows).n;
     if (n > 0) {
         f.n = n;
         f.pairs = (long long)n * a.group;
-        f.tiles = (int)((f.pairs + BT_PAIRS - 1) / BT_PAIRS);
+        f.tiles = whole ? 1 : battn_tiles(f.pairs);
         f.step = (long long)min(max(battn_len(a, r) - n, 0), BT_FAR) * a.group;
         f.small = (int)min((long long)f.tiles, max(f.block - f.step, 0ll) / BT_PAIRS);
     }
@@ -84,7 +86,9 @@ __device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r,
 
 // NP: 1 all in bf16; 3 fp32 queries over a bf16 cache, which stay exact as three bf16 planes, as do the weights; 0 all in fp32, on the fp32 matrix
 // instructions (two positions, or dimensions, each), which take keys, values and weights as they lie.
-// TREE (pages): of the new rows a row sees those that its mask has.
+// TREE (pages): of the new rows a row sees those that its mask has, looked at in the last blocks only, the mask's first word in registers. 24 trees of 8 to 64 rows at 200 to 4000
+// positions, 40 heads of 128 over 8, bf16: 86 us, 430 TFLOP/s; two of 60 to 64 rows at 100 000 positions: 350 us, 716 TFLOP/s. What bounds them is a block's own chain (arrival, products,
+// exponentials, products): a tile takes as long for 2 pairs as for 128.
 template <int HD, bool PAGED, int NP, bool TREE>
 __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void battn_tile_kernel(BattnArgs a) {
     static_assert(PAGED || !TREE, "");
@@ -99,20 +103,64 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
     const unsigned int flip = a.scale2 < 0.f ? 0x80000000u : 0u;
 
     int r = 0, kvh, tile;
-    TileShape f{0, 0, 0, 0, 0, 0};
+    TileShape f{0, 0, 0, false, 0, 0, 0};
     // the run: where it is and where it ends, in cost; the cost before the tile
     long long at = 0, end = 0, before = 0, run_q = 0, run_rem = 0;
-    int run = 0;
+    int run = 0;                                              // (its place among the runs that may hold parts of the same tiles)
+    int slot_run = 0;                                         // its place in the workspace
     const long long block_cost = (long long)CH * a.group;
+    // Trees: the tiles of a kv head side by side, each in a workgroup of its own over the same positions, so that what one of them reads is in the die's L2 for the others. Then a
+    // run is a stretch of positions, and as many workgroups of one die share it as the batch's widest request has tiles.
+    bool whole = false;
+    int mine_of = 0, most_runs = (int)gridDim.x;              // this workgroup's tile; runs at most
     if constexpr (PAGED) {
-        run = battn_run();
-        if (tid == 0) ((FewMerge *)a.ws)[run] = FewMerge{0, 0, 0, 0, 0};
+        run = slot_run = battn_run();
+        if constexpr (TREE) {
+            long long one = 0, all = 0;                       // what a run's workgroups have to do if they are as many as the widest request's tiles, and what of it is work
+            int widest = 0;
+            for (int q0 = 0; q0 < a.n_requests; q0 += 64) {
+                long long cost = 0;
+                int tiles = 0;
+                if (q0 + lane < a.n_requests) {
+                    const TileShape g = battn_tile_shape(a, q0 + lane, CH, true);
+                    cost = g.total();
+                    tiles = battn_tiles(g.pairs);
+                }
+                long long tiled = cost * tiles;
+                for (int off = 32; off; off >>= 1) {
+                    cost += __shfl_xor(cost, off);
+                    tiled += __shfl_xor(tiled, off);
+                    tiles = max(tiles, __shfl_xor(tiles, off));
+                }
+                one += cost;
+                all += tiled;
+                widest = max(widest, tiles);
+            }
+            one = battn_same(one);
+            all = battn_same(all);
+            widest = battn_same(widest);
+            // (only where three quarters of those workgroups have a tile: two requests of 60 to 64 rows at 100 000 positions, three tiles, 393 -> 350 us; 24 requests of 8 to 64 rows,
+            // one to three tiles, 64 % of them, 86 -> 125)
+            whole = widest > 1 && widest <= 8 && all * 4 >= one * widest * 3;
+            if (whole) {
+                const int slots = gridDim.x >> 3, per = slots / widest, die = blockIdx.x & 7, slot = blockIdx.x >> 3;
+                most_runs = 8 * per;
+                mine_of = slot % widest;
+                run = die * per + slot / widest;
+                slot_run = mine_of * most_runs + run;
+                if (slot >= per * widest) {                   // (left over)
+                    slot_run = most_runs * widest + die * (slots - per * widest) + slot - per * widest;
+                    run = INT_MAX;
+                }
+            }
+        }
+        if (tid == 0) ((FewMerge *)a.ws)[slot_run] = FewMerge{0, 0, 0, 0, 0};
         long long total = 0;
         for (int pass = 0; pass < 2; ++pass) {
             bool found = false;
             for (int q0 = 0; q0 < a.n_requests && !found; q0 += 64) {
                 long long upto = 0;
-                if (q0 + lane < a.n_requests) upto = battn_tile_shape(a, q0 + lane, CH).total() * a.Hkv;
+                if (q0 + lane < a.n_requests) upto = battn_tile_shape(a, q0 + lane, CH, whole).total() * a.Hkv;
                 for (int off = 1; off < 64; off <<= 1) {
                     const long long u = __shfl_up(upto, off);
                     if (lane >= off) upto += u;
@@ -120,7 +168,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
                 if (pass == 0) total += battn_lane(upto, 63);
                 if (pass == 0 && q0 + 64 >= a.n_requests) {   // the total is known
                     if (total == 0) return;
-                    const int runs = battn_same((int)max(1ll, min((long long)gridDim.x, battn_divide(total, block_cost))));
+                    const int runs = battn_same((int)max(1ll, min((long long)most_runs, battn_divide(total, block_cost))));
                     if (run >= runs) return;
                     run_q = battn_divide(total, runs);
                     run_rem = total - run_q * runs;
@@ -141,7 +189,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
             }
             if (found) break;
         }
-        f = battn_tile_shape(a, r, CH);
+        f = battn_tile_shape(a, r, CH, whole);
         kvh = (int)battn_divide(at - before, f.total());
         before += kvh * f.total();
         int lo = 0, hi = f.tiles;
@@ -212,7 +260,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
         len = PAGED ? battn_same(battn_len(a, r)) : n;
         last = len - 1;
         base = len - n;                                       // position of the request's first new row
-        const int tile_last = battn_same((int)((min((long long)(tile + 1) * BT_PAIRS, f.pairs) - 1) / a.group));
+        const int tile_last = battn_same((int)(((whole ? f.pairs : min((long long)(tile + 1) * BT_PAIRS, f.pairs)) - 1) / a.group));
         n_blocks = (max(base, 0) + tile_last) / CH + 1;
         b0 = 0;
         b1 = n_blocks;
@@ -236,9 +284,32 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
             look_up(b0 + 1);
         }
     };
+    // on to the next tile; false behind the run's last
+    auto advance = [&]() __attribute__((always_inline)) {
+        before = battn_same(before + f.cost(tile));
+        bool goes_on = before < end;
+        if (goes_on) {
+            at = before;
+            if (++tile == f.tiles) {
+                tile = 0;
+                if (++kvh == a.Hkv) {
+                    kvh = 0;
+                    do {
+                        if (++r >= a.n_requests) goes_on = false;     // (never: the run lies in some requests)
+                        else f = battn_tile_shape(a, r, CH, whole);
+                    } while (goes_on && f.tiles == 0);
+                }
+            }
+        }
+        return goes_on;
+    };
+    if constexpr (TREE) {
+        while (whole && mine_of >= battn_tiles(f.pairs))      // the request has no such tile
+            if (!advance()) return;
+    }
     enter();
     while (b0 < b1) {
-        const long long p0 = (long long)tile * BT_PAIRS;
+        const long long p0 = (long long)(whole ? mine_of : tile) * BT_PAIRS;
         const int wave_first = battn_same((int)((p0 + wave * 32) / a.group));                                     // the wavefront's first row
         const int wave_last = battn_same(p0 + wave * 32 < f.pairs ? (int)((min(p0 + wave * 32 + 32, f.pairs) - 1) / a.group) : INT_MIN / 2);      // ... and last one
         const long long pair = min(p0 + wave * 32 + col, f.pairs - 1);
@@ -413,28 +484,16 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
         bool goes_on = false;
         if constexpr (PAGED) {
             if (!whole && b0 == 0 && tid == 0)                // it goes on in the runs behind this one
-                ((FewMerge *)a.ws)[run] = FewMerge{battn_run_of(before + f.cost(tile) - 1, run_q, run_rem) - run + 1, r0, kvh,
-                                                   tile * BT_PAIRS, (int)min((long long)BT_PAIRS, f.pairs - p0)};
+                ((FewMerge *)a.ws)[slot_run] = FewMerge{battn_run_of(before + f.cost(tile) - 1, run_q, run_rem) - run + 1, r0, kvh,
+                                                        (int)p0, (int)min((long long)BT_PAIRS, f.pairs - p0)};
         }
-        const int slot = 2 * run + (b0 == 0);
+        const int slot = 2 * slot_run + (b0 == 0);
         // on to the next tile: its first block is on its way while this one is written (the buffer that it goes to has been read by all)
         if constexpr (PAGED) {
-            before = battn_same(before + f.cost(tile));
-            goes_on = before < end;
-            if (goes_on) {
-                at = before;
-                if (++tile == f.tiles) {
-                    tile = 0;
-                    if (++kvh == a.Hkv) {
-                        kvh = 0;
-                        do {
-                            if (++r >= a.n_requests) goes_on = false;     // (never: the run lies in some requests)
-                            else f = battn_tile_shape(a, r, CH);
-                        } while (goes_on && f.tiles == 0);
-                    }
-                }
-                if (goes_on) enter();
-            }
+            goes_on = advance();
+            if constexpr (TREE)
+                while (goes_on && whole && mine_of >= battn_tiles(f.pairs)) goes_on = advance();
+            if (goes_on) enter();
         }
         if (!live) {
         } else if (!PAGED || whole) {

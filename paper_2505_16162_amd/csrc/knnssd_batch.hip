@@ -89,7 +89,8 @@ template <int HD, int NP>
 static void launch_merge(const BattnArgs &a, unsigned runs, int pairs, int64_t groups, int slot_pairs, hipStream_t s) {
     // few groups lie in many runs each, whose pairs then take four teams of lanes
     const int at_once = groups < BF_WGS / 4 ? battn_merge_teams<HD>() / 4 : battn_merge_teams<HD>();
-    hipLaunchKernelGGL((battn_merge_kernel<HD, NP>), dim3(runs, (pairs + at_once - 1) / at_once), dim3(BM_NT), 0, s, a, slot_pairs);
+    const unsigned most = groups < BF_WGS / 4 && groups < runs ? (unsigned)groups : runs;
+    hipLaunchKernelGGL((battn_merge_kernel<HD, NP>), dim3(most, (pairs + at_once - 1) / at_once), dim3(BM_NT), 0, s, a, slot_pairs, (int)runs);
 }
 
 // tiles at most; what is too much ends at once
@@ -114,11 +115,23 @@ static void launch_prompt_tiles(const BattnArgs &a, hipStream_t s) {
 // Two requests of 20 to 30 pairs at 100 000 positions 223 / 157; 227 / 167. The bound is the caller's most_rows, or all rows of the batch.
 static const int FEW_PAIRS = 16;
 
+// what battn_few_kernel has to do, at most: blocks of positions for every group of pairs
+template <int HD> static int64_t few_units(const BattnArgs &a, int64_t groups) {
+    const int ch = battn_few_positions<HD>();
+    const int64_t blocks = (((int64_t)a.width << a.shift) + ch - 1) / ch;
+    return blocks < INT32_MAX ? blocks * groups * a.Hkv : INT64_MAX;
+}
+static int64_t few_groups(const BattnArgs &a) { return ((int64_t)a.n_rows * a.group + FEW_PAIRS - 1) / FEW_PAIRS + a.n_requests; }
+
+// Trees have many pairs from the start, but few trees over short contexts are done before a tile's first block is: whole calls, us, battn_few_kernel / tiles, one request, 40 heads of 128 over 8, bf16:
+//   26 rows over 400 positions 16 / 25, 1500 21 / 24, 3000 (7600 units) 24 / 27, 6000 (15 000) 30 / 29; 60 rows 400 16 / 26, 1500 (8400) 23 / 28, 3000 (16 000) 31 / 31, 6000 44 / 33
+//   40 heads over 40: 60 rows over 1500 (9900) 24 / 28; four requests of 26 rows over 1500 (15 000) 30 / 29
+// The positions are those that the table can hold.
+static const int64_t FEW_UNITS = 12288;
+
 template <int HD, int NP, bool TREE>
 static void launch_few(const BattnArgs &a, int64_t most, hipStream_t s) {
-    const int ch = battn_few_positions<HD>();
-    const int64_t blocks = (((int64_t)a.width << a.shift) + ch - 1) / ch, groups = ((int64_t)a.n_rows * a.group + FEW_PAIRS - 1) / (FEW_PAIRS) + a.n_requests;
-    const int64_t units = blocks < INT32_MAX ? blocks * groups * a.Hkv : INT64_MAX;      // at most
+    const int64_t groups = few_groups(a), units = few_units<HD>(a, groups);      // at most
     const unsigned runs = (unsigned)(units / 4 + 1 < BF_WGS ? (units / 4 + 8) & -8 : BF_WGS);
     hipLaunchKernelGGL((battn_few_kernel<HD, NP, TREE>), dim3(runs), dim3(256), 0, s, a);
     launch_merge<HD, NP>(a, runs, (int)(most < FEW_PAIRS ? most : FEW_PAIRS), groups * a.Hkv, FEW_PAIRS, s);
@@ -136,7 +149,7 @@ static void launch_paged(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, in
     if (kv_dtype == KNNSSD_FP32) {
         if (rows_alone(a, (int64_t)a.width << a.shift)) hipLaunchKernelGGL((battn_row_kernel<HD, true, TREE>), dim3((unsigned)(a.n_rows * a.H)), dim3(256), 0, s, a);
         else launch_paged_tiles<HD, 0, TREE>(a, most, s);
-    } else if (most <= FEW_PAIRS) {
+    } else if (most <= FEW_PAIRS || (TREE && few_units<HD>(a, few_groups(a)) <= FEW_UNITS)) {
         if (dtype == KNNSSD_FP32) launch_few<HD, 3, TREE>(a, most, s);
         else launch_few<HD, 1, TREE>(a, most, s);
     } else {
