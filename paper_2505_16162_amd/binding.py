@@ -483,7 +483,8 @@ def knnssd_tree_verify(logits: torch.Tensor, tokens: torch.Tensor, parents: torc
                        stream: Optional[torch.cuda.Stream] = None):
     """Drafted tokens tried against softmax(logits / temperature): (path, n_path, next_token). logits [rows][vocab], tokens and parents int32 [rows], temperature and u_next
     float32 [requests], u_accept float32 [rows], the numbers uniform on [0, 1). draft_logits: those that each row's children were drawn from (with the same temperature); None: the drafts were not
-    drawn. path int32 [rows]: a request's rows that were taken, at its first rows' places, -1 behind; n_path, next_token int32 [requests]; made, of `stream`, where they are not given."""
+    drawn. path int32 [rows]: a request's rows that were taken, at its first rows' places, -1 behind; n_path, next_token int32 [requests]. Those that are not given are made, of `stream`;
+    path's rows behind the last request's then hold whatever was there. most_children: an upper bound of a row's children if the caller has one, else 0; it only chooses the kernels."""
     dev, n, rows = _on_a_gpu(logits, "logits"), row_start.numel() - 1, tokens.numel()
     lp, ls = _logits(logits, dev, "logits")
     dp, ds = (None, 0) if draft_logits is None else _logits(draft_logits, dev, "draft_logits")
