@@ -444,7 +444,7 @@ int32_t knnssd_tree_verify(const void *logits_dev, int64_t logits_stride, const 
 
 /* The path's keys and values side by side: in every one of n_blocks caches (alike in everything but their addresses: KNNSSD_ESHAPE) the entry of row path[row_start[r] + j] of request r goes to position
  * kv_len[r] - rows + j, for j < n_path[r]; cached_dev[r] becomes the position behind the last of them, the next knnssd_page_plan's `cached`. A path ascends strictly; it ends before an entry that does
- * not, that is no row of the request or that lies beyond its table. What a request's positions from cached[r] on hold afterwards is of no use. cached_dev must not overlap kv_len_dev or n_path_dev (KNNSSD_EINVAL).
+ * not, that is no row of the request or that lies beyond its table. What a request's positions from cached[r] on hold afterwards is of no use. cached_dev must not overlap an input (KNNSSD_EINVAL).
  * KNNSSD_ERANGE for n_blocks outside [1, 65535], table_width < 1, n_requests or n_rows as in knnssd_tree_plan. */
 int32_t knnssd_tree_keep(const knnssd_pages *blocks, int32_t n_blocks, const int32_t *block_table_dev, int32_t table_width, const int32_t *row_start_dev,
                          const int32_t *kv_len_dev, int32_t n_requests, int32_t n_rows, const int32_t *path_dev, const int32_t *n_path_dev,

@@ -518,7 +518,7 @@ class PageBlocks:
 def knnssd_tree_keep(blocks: PageBlocks, block_table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor, path: torch.Tensor, n_path: torch.Tensor,
                      cached: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """The keys and values of the rows on each request's path (knnssd_tree_verify) to the positions behind its cached ones, in all blocks; cached (int32 [requests]) becomes
-    the requests' new lengths. It must not be kv_len or n_path."""
+    the requests' new lengths. It must not be one of the inputs."""
     dev = blocks.device
     if block_table.dim() != 2:
         raise ValueError("block_table must be [n_requests][table_width]")

@@ -112,8 +112,10 @@ extern "C" int32_t knnssd_tree_keep(const knnssd_pages *blocks, int32_t n_blocks
             return KNNSSD_ESHAPE;
     }
     // (the workgroups of other blocks read a request's lengths when the first one may have written what is left of them)
-    for (const int32_t *in : {kv_len_dev, n_path_dev})
-        if (cached_dev < in + n_requests && in < cached_dev + n_requests) return KNNSSD_EINVAL;
+    const struct { const int32_t *at; int64_t n; } inputs[] = {{kv_len_dev, n_requests}, {n_path_dev, n_requests}, {row_start_dev, n_requests + 1}, {path_dev, n_rows},
+                                                               {block_table_dev, (int64_t)n_requests * table_width}};
+    for (const auto &in : inputs)
+        if (cached_dev < in.at + in.n && in.at < cached_dev + n_requests) return KNNSSD_EINVAL;
     const int64_t elt = dtype_bytes(p.kv_dtype);
     TreeKeepArgs a{};
     a.page_stride = p.page_stride * elt; a.head_stride = p.head_stride * elt; a.pos_stride = p.pos_stride * elt;

@@ -79,7 +79,9 @@ def test_workspace_of_the_verification(lib):
 
 @pytest.mark.parametrize("kw,code", [(dict(table=None), EINVAL), (dict(row_start=None), EINVAL), (dict(kv_len=None), EINVAL), (dict(path=None), EINVAL), (dict(n_path=None), EINVAL),
                                      (dict(cached=None), EINVAL), (dict(n_blocks=0), ERANGE), (dict(n_blocks=65536), ERANGE), (dict(width=0), ERANGE), (dict(n=0), ERANGE),
-                                     (dict(n=4097), ERANGE), (dict(rows=0), ERANGE), (dict(cached=A), EINVAL), (dict(cached=A + 4), EINVAL), (dict(cached=2 * A - 4), EINVAL)])
+                                     (dict(n=4097), ERANGE), (dict(rows=0), ERANGE), (dict(cached=A), EINVAL), (dict(cached=A + 4), EINVAL), (dict(cached=2 * A - 4), EINVAL),
+                                     (dict(cached=5 * A, path=5 * A - 16), EINVAL), (dict(cached=5 * A, row_start=5 * A - 8), EINVAL),
+                                     (dict(cached=5 * A, table=5 * A - 28), EINVAL)])
 def test_keep(lib, kw, code):
     p = pages()
     assert call(lib.knnssd_tree_keep, dict(KEEP, blocks=(binding.PagesStruct * 2)(p, p)), kw) == code
