@@ -89,8 +89,9 @@ template <int HD, int NP>
 static void launch_merge(const BattnArgs &a, unsigned runs, int pairs, int64_t groups, int slot_pairs, hipStream_t s) {
     // few groups lie in many runs each, whose pairs then take four teams of lanes
     const int at_once = groups < BF_WGS / 4 ? battn_merge_teams<HD>() / 4 : battn_merge_teams<HD>();
-    const unsigned most = groups < BF_WGS / 4 && groups < runs ? (unsigned)groups : runs;
-    hipLaunchKernelGGL((battn_merge_kernel<HD, NP>), dim3(most, (pairs + at_once - 1) / at_once), dim3(BM_NT), 0, s, a, slot_pairs, (int)runs);
+    const unsigned tall = (pairs + at_once - 1) / at_once;
+    const bool search = groups < BF_WGS / 4 && groups < runs && runs * tall > 4096;      // (the search takes 1 us, 4096 places that end at once 1.5)
+    hipLaunchKernelGGL((battn_merge_kernel<HD, NP>), dim3(search ? (unsigned)groups : runs, tall), dim3(BM_NT), 0, s, a, slot_pairs, (int)runs);
 }
 
 // tiles at most; what is too much ends at once
