@@ -348,18 +348,42 @@ __global__ __launch_bounds__(256) void tv_stats_kernel(TvArgs a) {
     if (lane == 0) a.stats[(size_t)(draft ? a.n_rows : 0) * a.chunks + unit] = TvStat{bad ? 0.f : top, first, bad ? (double)NAN : sum};
 }
 
-// a row's chunks put together by a group of `width` lanes
+// a row's chunks put together by a group of `width` lanes, four chunks a lane at a time
 __device__ __forceinline__ TvRow tv_join(const TvStat *s, int chunks, double k, int in, int width) {
+    constexpr int U = 4;
     TvRow row{-INFINITY, INT32_MAX, 0.0};
-#pragma unroll 8
-    for (int c = in; c < chunks; c += width) row.top = fmaxf(row.top, s[c].top);
-    row.top = tv_max(row.top, width);
-#pragma unroll 4
-    for (int c = in; c < chunks; c += width) {
-        const TvStat one = s[c];
-        if (one.top > -INFINITY) row.sum += one.sum * tv_exp2(((double)one.top - row.top) * k);
-        else if (one.sum != one.sum) row.sum = one.sum;
-        if (one.top == row.top) row.first = min(row.first, one.first);
+    for (int c0 = in; c0 - in < chunks; c0 += U * width) {    // (the same number of times for all of the group)
+        float top[U], most = row.top;
+        int first[U];
+        double sum[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int c = c0 + j * width;
+            top[j] = -INFINITY;
+            first[j] = INT32_MAX;
+            sum[j] = 0.0;
+            if (c < chunks) {
+                const TvStat one = s[c];
+                top[j] = one.top;
+                first[j] = one.first;
+                sum[j] = one.sum;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) most = fmaxf(most, top[j]);
+        most = tv_max(most, width);
+        if (most > row.top) {
+            if (row.top > -INFINITY) row.sum *= tv_exp2(((double)row.top - most) * k);
+            row.top = most;
+            row.first = INT32_MAX;
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            if (j > 0 && c0 - in + j * width >= chunks) break;
+            if (top[j] > -INFINITY) row.sum += sum[j] * tv_exp2(((double)top[j] - row.top) * k);
+            else if (sum[j] != sum[j]) row.sum = sum[j];
+            if (top[j] == row.top) row.first = min(row.first, first[j]);
+        }
     }
     row.sum = tv_sum(row.sum, width);
     row.first = tv_min(row.first, width);
@@ -519,10 +543,11 @@ __global__ __launch_bounds__(TV_NT) void tv_walk_kernel(TvArgs a, int round, int
                 for (int x = lane; x < a.chunks; x += 64) left += chunk_sum[x];
                 left = tv_sum(left);
             }
-            // a lane has a row of the 64 that the walk is among
+            // a lane has a row of the 64 that the walk is among: whether it is taken if it is the first that is tried, whether it has children, a distribution
             int seg = -1, par = -1, tok = 0;
             float u_of = 0.f;
             double p_of = 0.0, q_of = 1.0;
+            unsigned long long taken = 0, with_children = 0, without_one = 0;
             auto among = [&](int s) __attribute__((always_inline)) {
                 seg = s;
                 const int i = min(s * 64 + lane, n - 1);
@@ -531,10 +556,15 @@ __global__ __launch_bounds__(TV_NT) void tv_walk_kernel(TvArgs a, int round, int
                 u_of = __int_as_float(u_bits[i]);
                 p_of = p_at[i];
                 if (drawn) q_of = q_at[i];
+                const bool children = inner[i];
+                taken = __ballot(p_of > u_of * q_of);
+                with_children = __ballot(children);
+                without_one = __ballot(p_row[i].top != p_row[i].top || (drawn && children && q_row[i].top != q_row[i].top));
             };
-            among(last >> 6);
-            bool goes_on = inner[node];
-            lost = p_row[node].top != p_row[node].top || (drawn && goes_on && q_row[node].top != q_row[node].top);
+            among(node >> 6);
+            bool goes_on = with_children >> (node & 63) & 1;
+            lost = without_one >> (node & 63) & 1;
+            if (last >> 6 > seg) among(last >> 6);
             while (!waits && !lost && goes_on) {
                 const unsigned long long match = __ballot(par == node && seg * 64 + lane > last);
                 if (!match) {
@@ -543,24 +573,31 @@ __global__ __launch_bounds__(TV_NT) void tv_walk_kernel(TvArgs a, int round, int
                     continue;
                 }
                 const int l = __builtin_ctzll(match), child = seg * 64 + l;
+                const bool untried = c == 0.0 && left == 1.0;
                 last = child;
-                const double u = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u_of), l)), qx = tv_lane(q_of, l);
-                double px = tv_lane(p_of, l);
-                if (!drawn) {                                 // the same token again: it has been rejected
-                    const int x = __builtin_amdgcn_readlane(tok, l);
-                    if (__any(par == node && tok == x && lane < l)) px = 0.0;
-                    for (int i = (node & ~63) + lane; i < seg * 64; i += 64)
-                        if (__any(parent[i] == node && token[i] == x)) px = 0.0;
+                bool take = taken >> l & 1;
+                double px = 0.0, qx = 1.0;
+                if (!untried || !take) {
+                    const double u = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u_of), l));
+                    px = tv_lane(p_of, l);
+                    qx = tv_lane(q_of, l);
+                    if (!drawn && !untried) {                 // the same token again: it has been rejected
+                        const int x = __builtin_amdgcn_readlane(tok, l);
+                        if (__any(par == node && tok == x && lane < l)) px = 0.0;
+                        for (int i = (node & ~63) + lane; i < seg * 64; i += 64)
+                            if (__any(parent[i] == node && token[i] == x)) px = 0.0;
+                    }
+                    take = px > (c + u * left) * qx;
                 }
-                if (px > (c + u * left) * qx) {
+                if (take) {
                     node = child;
                     if (lane == 0) a.path[rows.first + kept] = child;
                     ++kept;
                     c = 0.0;
                     left = 1.0;
                     summed = false;
-                    goes_on = inner[node];
-                    lost = p_row[node].top != p_row[node].top || (drawn && goes_on && q_row[node].top != q_row[node].top);
+                    goes_on = with_children >> l & 1;
+                    lost = without_one >> l & 1;
                 } else if (!drawn) {
                     left -= px;
                 } else if (qx > 0.0) {                        // (a token that the draft cannot have drawn says nothing about its distribution)
@@ -729,8 +766,9 @@ __global__ __launch_bounds__(TV_NT) void tv_walk_kernel(TvArgs a, int round, int
             if (mine == INT32_MAX && run > target) mine = at + e;
         }
     }
-    mine = tv_min(mine);
-    with = -tv_min(-with);
+    const unsigned long long past = __ballot(mine != INT32_MAX), any = __ballot(with >= 0);       // (tokens are in the order of the lanes)
+    mine = past ? __builtin_amdgcn_readlane(mine, __builtin_ctzll(past)) : INT32_MAX;
+    with = any ? __builtin_amdgcn_readlane(with, 63 - __builtin_clzll(any)) : -1;
     if (lane == 0) {
         found[wave] = mine;
         held[wave] = with;
