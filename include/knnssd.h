@@ -409,7 +409,7 @@ int32_t knnssd_context_pages(const knnssd_ctx *ctx, int32_t block, int32_t page_
 /* Positions and masks of ancestors. positions_dev [n_rows]: kv_len[r] minus the request's rows plus the row's depth (a root's is 0), over those that knnssd_page_plan wrote (a row's slot stays: the
  * tree's rows lie in the cache in their own order). masks_dev [n_rows][mask_words], 8-byte aligned: bit j % 64 of word j / 64 says that the row sees row j of its request: itself and its ancestors. A
  * request has up to 64 * mask_words rows; the masks of further ones are 0 and their positions -1. Rows behind the last request's are left as they were. row_start_dev and kv_len_dev as
- * knnssd_page_plan wrote them. KNNSSD_ERANGE for mask_words outside [1, KNNSSD_MAX_TREE / 64], n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows outside [1, KNNSSD_MAX_ROW_HEADS / 4]. */
+ * knnssd_page_plan wrote them. Outputs must not overlap inputs or each other (KNNSSD_EINVAL). KNNSSD_ERANGE for mask_words outside [1, KNNSSD_MAX_TREE / 64], n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows outside [1, KNNSSD_MAX_ROW_HEADS / 4]. */
 int32_t knnssd_tree_plan(const int32_t *parents_dev, const int32_t *row_start_dev, const int32_t *kv_len_dev, int32_t n_requests, int32_t n_rows,
                          int32_t *positions_dev, uint64_t *masks_dev, int32_t mask_words, void *hip_stream);
 
@@ -435,7 +435,8 @@ int32_t knnssd_tree_attention(const knnssd_pages *pages, const int32_t *block_ta
  * KNNSSD_MAX_TREE on of a request are none of the tree. most_children: an upper bound of a row's children if the caller has one, else 0; it only chooses the kernels.
  * ws_dev: knnssd_tree_verify_bytes (drawn: draft_logits_dev is given; 0: sizes that the call refuses), 256-byte aligned, of any contents; nothing in it outlives a call. The same call gives the same result.
  * KNNSSD_ESHAPE for vocab outside [1, KNNSSD_MAX_VOCAB], KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows outside [1, KNNSSD_MAX_ROW_HEADS / 4] or
- * n_rows * ceil(vocab / 2048) > KNNSSD_MAX_ROW_HEADS. Outputs must not overlap inputs. */
+ * n_rows * ceil(vocab / 2048) > KNNSSD_MAX_ROW_HEADS. Outputs must not overlap the int32 and float inputs or each other
+ * (KNNSSD_EINVAL), nor what else is read. */
 size_t knnssd_tree_verify_bytes(int32_t n_rows, int32_t n_requests, int32_t vocab, int32_t drawn);
 int32_t knnssd_tree_verify(const void *logits_dev, int64_t logits_stride, const void *draft_logits_dev, int64_t draft_stride, int32_t dtype, int32_t vocab,
                            const int32_t *tokens_dev, const int32_t *parents_dev, const int32_t *row_start_dev, int32_t n_requests, int32_t n_rows,
@@ -444,8 +445,8 @@ int32_t knnssd_tree_verify(const void *logits_dev, int64_t logits_stride, const 
 
 /* The path's keys and values side by side: in every one of n_blocks caches (alike in everything but their addresses: KNNSSD_ESHAPE) the entry of row path[row_start[r] + j] of request r goes to position
  * kv_len[r] - rows + j, for j < n_path[r]; cached_dev[r] becomes the position behind the last of them, the next knnssd_page_plan's `cached`. A path ascends strictly; it ends before an entry that does
- * not, that is no row of the request or that lies beyond its table. What a request's positions from cached[r] on hold afterwards is of no use. cached_dev must not overlap an input (KNNSSD_EINVAL).
- * KNNSSD_ERANGE for n_blocks outside [1, 65535], table_width < 1, n_requests or n_rows as in knnssd_tree_plan. */
+ * not, that is no row of the request or that lies beyond its table. What a request's positions from cached[r] on hold afterwards is of no use. cached_dev must not overlap an input, and no cache be given twice, as keys
+ * and values of one block or in two blocks that share one (KNNSSD_EINVAL). KNNSSD_ERANGE for n_blocks outside [1, 1024], table_width < 1, n_requests or n_rows as in knnssd_tree_plan. */
 int32_t knnssd_tree_keep(const knnssd_pages *blocks, int32_t n_blocks, const int32_t *block_table_dev, int32_t table_width, const int32_t *row_start_dev,
                          const int32_t *kv_len_dev, int32_t n_requests, int32_t n_rows, const int32_t *path_dev, const int32_t *n_path_dev,
                          int32_t *cached_dev, void *hip_stream);

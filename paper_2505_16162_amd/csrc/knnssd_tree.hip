@@ -1,12 +1,17 @@
 // Host side of the calls for trees of drafted tokens: plan, verification, keeping a path. (Attention: knnssd_batch.hip.)
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <functional>
+
 #include "hip_try.h"
 #include "kernels_tree.h"
 #include "kernels_tverify.h"
 #include "pages_check.h"
 
 using namespace ks;
+
+static const int KEEP_MOST_BLOCKS = 1024;                     // what a cache that is given twice is looked for among
 
 static const_ints ints(const int32_t *p) { return (const_ints)(uintptr_t)p; }
 
@@ -16,11 +21,29 @@ static int32_t batch_check(const int32_t *row_start_dev, int32_t n_requests, int
     return n_requests < 1 || n_requests > KNNSSD_MAX_REQUESTS || n_rows < 1 || n_rows > KNNSSD_MAX_ROW_HEADS / 4 ? KNNSSD_ERANGE : KNNSSD_OK;
 }
 
+// Whether an output has entries of an input (or another output): workgroups of other requests would read them before or after.
+struct Ints { const void *at; int64_t n; int bytes = 4; };
+static bool overlap(const Ints &a, const Ints &b) {
+    const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+    return x < y + (uintptr_t)(b.n * b.bytes) && y < x + (uintptr_t)(a.n * a.bytes);
+}
+template <int OUT, int IN> static bool overlap(const Ints (&out)[OUT], const Ints (&in)[IN]) {
+    for (int o = 0; o < OUT; ++o) {
+        for (const Ints &i : in)
+            if (overlap(out[o], i)) return true;
+        for (int x = 0; x < o; ++x)
+            if (overlap(out[o], out[x])) return true;
+    }
+    return false;
+}
+
 extern "C" int32_t knnssd_tree_plan(const int32_t *parents_dev, const int32_t *row_start_dev, const int32_t *kv_len_dev, int32_t n_requests, int32_t n_rows,
                                     int32_t *positions_dev, uint64_t *masks_dev, int32_t mask_words, void *hip_stream) {
     if (!parents_dev || !kv_len_dev || !positions_dev || !masks_dev || ((uintptr_t)masks_dev & 7)) return KNNSSD_EINVAL;
     KS_TRY(batch_check(row_start_dev, n_requests, n_rows));
     if (!mask_words_ok(mask_words)) return KNNSSD_ERANGE;
+    const Ints out[] = {{positions_dev, n_rows}, {masks_dev, (int64_t)n_rows * mask_words, 8}}, in[] = {{parents_dev, n_rows}, {row_start_dev, n_requests + 1}, {kv_len_dev, n_requests}};
+    if (overlap(out, in)) return KNNSSD_EINVAL;
     TreePlanArgs a{};
     a.parents = parents_dev; a.row_start = ints(row_start_dev); a.kv_len = ints(kv_len_dev); a.masks = (unsigned long long *)masks_dev; a.positions = positions_dev;
     a.n_rows = n_rows; a.words = mask_words;
@@ -82,6 +105,9 @@ extern "C" int32_t knnssd_tree_verify(const void *logits_dev, int64_t logits_str
     if (most_children < 0) return KNNSSD_ERANGE;
     if (!values_ok(logits_dev, logits_stride, vocab, dtype) || (draft_logits_dev && !values_ok(draft_logits_dev, draft_stride, vocab, dtype))) return KNNSSD_EINVAL;
     if (((uintptr_t)ws_dev & 255) || ws_bytes < knnssd_tree_verify_bytes(n_rows, n_requests, vocab, draft_logits_dev != nullptr)) return KNNSSD_EINVAL;
+    const Ints out[] = {{path_dev, n_rows}, {n_path_dev, n_requests}, {next_token_dev, n_requests}};
+    const Ints in[] = {{tokens_dev, n_rows}, {parents_dev, n_rows}, {row_start_dev, n_requests + 1}, {temperature_dev, n_requests}, {u_accept_dev, n_rows}, {u_next_dev, n_requests}};
+    if (overlap(out, in)) return KNNSSD_EINVAL;
     const TvLayout l = tv_layout(n_rows, n_requests, vocab, draft_logits_dev != nullptr);
     TvArgs a{};
     a.logits = logits_dev; a.draft = draft_logits_dev; a.logits_stride = logits_stride; a.draft_stride = draft_stride;
@@ -102,7 +128,7 @@ extern "C" int32_t knnssd_tree_keep(const knnssd_pages *blocks, int32_t n_blocks
                                     int32_t *cached_dev, void *hip_stream) {
     if (!blocks || !block_table_dev || !kv_len_dev || !path_dev || !n_path_dev || !cached_dev) return KNNSSD_EINVAL;
     KS_TRY(batch_check(row_start_dev, n_requests, n_rows));
-    if (n_blocks < 1 || n_blocks > 65535 || table_width < 1) return KNNSSD_ERANGE;
+    if (n_blocks < 1 || n_blocks > KEEP_MOST_BLOCKS || table_width < 1) return KNNSSD_ERANGE;
     const knnssd_pages &p = blocks[0];
     for (int i = 0; i < n_blocks; ++i) {
         const knnssd_pages &o = blocks[i];
@@ -112,10 +138,14 @@ extern "C" int32_t knnssd_tree_keep(const knnssd_pages *blocks, int32_t n_blocks
             return KNNSSD_ESHAPE;
     }
     // (the workgroups of other blocks read a request's lengths when the first one may have written what is left of them)
-    const struct { const int32_t *at; int64_t n; } inputs[] = {{kv_len_dev, n_requests}, {n_path_dev, n_requests}, {row_start_dev, n_requests + 1}, {path_dev, n_rows},
-                                                               {block_table_dev, (int64_t)n_requests * table_width}};
-    for (const auto &in : inputs)
-        if (cached_dev < in.at + in.n && in.at < cached_dev + n_requests) return KNNSSD_EINVAL;
+    const Ints out[] = {{cached_dev, n_requests}};
+    const Ints in[] = {{kv_len_dev, n_requests}, {n_path_dev, n_requests}, {row_start_dev, n_requests + 1}, {path_dev, n_rows}, {block_table_dev, (int64_t)n_requests * table_width}};
+    if (overlap(out, in)) return KNNSSD_EINVAL;
+    // (a cache that is given twice, as keys and values of one block or as two blocks that share theirs, would be moved twice, the second time what has been moved)
+    const void *bases[2 * KEEP_MOST_BLOCKS];
+    for (int i = 0; i < n_blocks; ++i) { bases[2 * i] = blocks[i].k_dev; bases[2 * i + 1] = blocks[i].v_dev; }
+    std::sort(bases, bases + 2 * n_blocks, std::less<const void *>());
+    if (std::adjacent_find(bases, bases + 2 * n_blocks) != bases + 2 * n_blocks) return KNNSSD_EINVAL;
     const int64_t elt = dtype_bytes(p.kv_dtype);
     TreeKeepArgs a{};
     a.page_stride = p.page_stride * elt; a.head_stride = p.head_stride * elt; a.pos_stride = p.pos_stride * elt;

@@ -24,17 +24,19 @@ def call(fn, base, kw):
     return fn(*[v for v in {**base, **kw}.values()])
 
 
-PLAN = dict(parents=A, row_start=A, kv_len=A, n=2, rows=5, positions=A, masks=A, words=1, stream=None)
+PLAN = dict(parents=A, row_start=A, kv_len=A, n=2, rows=5, positions=2 * A, masks=3 * A, words=1, stream=None)
 ATTENTION = dict(pages=None, table=A, width=4, row_start=A, kv_len=A, n=2, masks=A, words=1, q=A, qs=4 * 128, out=2 * A, os=4 * 128, dtype=1, rows=5, heads=4, scale=0.1,
                  most=0, ws=A, wsb=1 << 40, stream=None)
-VERIFY = dict(logits=A, ls=1000, draft=A, ds=1000, dtype=1, vocab=1000, tokens=A, parents=A, row_start=A, n=2, rows=5, temperature=A, u=A, u_next=A, path=A, n_path=A,
-              next_token=A, most=0, ws=A, wsb=1 << 40, stream=None)
+VERIFY = dict(logits=A, ls=1000, draft=A, ds=1000, dtype=1, vocab=1000, tokens=A, parents=A, row_start=A, n=2, rows=5, temperature=A, u=A, u_next=A, path=2 * A, n_path=3 * A,
+              next_token=4 * A, most=0, ws=A, wsb=1 << 40, stream=None)
 KEEP = dict(blocks=None, n_blocks=2, table=A, width=4, row_start=A, kv_len=A, n=2, rows=5, path=A, n_path=2 * A, cached=3 * A, stream=None)
 
 
 @pytest.mark.parametrize("kw,code", [(dict(parents=None), EINVAL), (dict(row_start=None), EINVAL), (dict(kv_len=None), EINVAL), (dict(positions=None), EINVAL),
                                      (dict(masks=None), EINVAL), (dict(masks=A + 4), EINVAL), (dict(words=0), ERANGE), (dict(words=17), ERANGE), (dict(words=-1), ERANGE),
-                                     (dict(n=0), ERANGE), (dict(n=4097), ERANGE), (dict(rows=0), ERANGE), (dict(rows=2 ** 23 + 1), ERANGE)])
+                                     (dict(n=0), ERANGE), (dict(n=4097), ERANGE), (dict(rows=0), ERANGE), (dict(rows=2 ** 23 + 1), ERANGE),
+                                     (dict(positions=A), EINVAL), (dict(positions=A - 16), EINVAL), (dict(masks=A + 8), EINVAL), (dict(kv_len=2 * A - 4), EINVAL),
+                                     (dict(positions=3 * A + 36), EINVAL), (dict(row_start=3 * A + 32), EINVAL)])
 def test_plan(lib, kw, code):
     assert call(lib.knnssd_tree_plan, PLAN, kw) == code
 
@@ -60,7 +62,8 @@ def test_pages_of_attention_and_keep(lib, kw, code):
     (dict(dtype=2), EINVAL), (dict(vocab=0), ESHAPE), (dict(vocab=-5), ESHAPE), (dict(vocab=2 ** 19 + 1, ls=2 ** 20, ds=2 ** 20), ESHAPE), (dict(ls=999), EINVAL), (dict(ds=999), EINVAL),
     (dict(ls=-1000), EINVAL), (dict(logits=A + 1), EINVAL), (dict(draft=A + 1), EINVAL), (dict(dtype=0, logits=A + 2), EINVAL), (dict(dtype=0, draft=A + 2), EINVAL), (dict(n=0), ERANGE),
     (dict(n=4097), ERANGE), (dict(rows=0), ERANGE), (dict(rows=2 ** 23 + 1), ERANGE), (dict(rows=2 ** 20, vocab=152064, ls=152064, ds=152064), ERANGE), (dict(most=-1), ERANGE),
-    (dict(ws=A + 128), EINVAL), (dict(wsb=255), EINVAL)])
+    (dict(ws=A + 128), EINVAL), (dict(wsb=255), EINVAL), (dict(path=A), EINVAL), (dict(path=A - 16), EINVAL), (dict(n_path=A + 16), EINVAL), (dict(next_token=A + 4), EINVAL),
+    (dict(tokens=4 * A - 16), EINVAL), (dict(u_next=3 * A + 4), EINVAL), (dict(n_path=2 * A + 16), EINVAL), (dict(next_token=3 * A - 4), EINVAL)])
 def test_verify(lib, kw, code):
     assert call(lib.knnssd_tree_verify, VERIFY, kw) == code
 
@@ -78,13 +81,19 @@ def test_workspace_of_the_verification(lib):
 
 
 @pytest.mark.parametrize("kw,code", [(dict(table=None), EINVAL), (dict(row_start=None), EINVAL), (dict(kv_len=None), EINVAL), (dict(path=None), EINVAL), (dict(n_path=None), EINVAL),
-                                     (dict(cached=None), EINVAL), (dict(n_blocks=0), ERANGE), (dict(n_blocks=65536), ERANGE), (dict(width=0), ERANGE), (dict(n=0), ERANGE),
+                                     (dict(cached=None), EINVAL), (dict(n_blocks=0), ERANGE), (dict(n_blocks=1025), ERANGE), (dict(width=0), ERANGE), (dict(n=0), ERANGE),
                                      (dict(n=4097), ERANGE), (dict(rows=0), ERANGE), (dict(cached=A), EINVAL), (dict(cached=A + 4), EINVAL), (dict(cached=2 * A - 4), EINVAL),
                                      (dict(cached=5 * A, path=5 * A - 16), EINVAL), (dict(cached=5 * A, row_start=5 * A - 8), EINVAL),
                                      (dict(cached=5 * A, table=5 * A - 28), EINVAL)])
 def test_keep(lib, kw, code):
-    p = pages()
-    assert call(lib.knnssd_tree_keep, dict(KEEP, blocks=(binding.PagesStruct * 2)(p, p)), kw) == code
+    blocks = (binding.PagesStruct * 2)(pages(), pages(k_dev=3 * A, v_dev=4 * A))
+    assert call(lib.knnssd_tree_keep, dict(KEEP, blocks=blocks), kw) == code
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(k_dev=3 * A), dict(v_dev=3 * A), dict(k_dev=2 * A, v_dev=3 * A), dict(k_dev=3 * A, v_dev=3 * A)])
+def test_keep_refuses_a_cache_that_is_given_twice(lib, kw):
+    """It would be moved twice: blocks that share their caches are given once, keys and values are two."""
+    assert call(lib.knnssd_tree_keep, dict(KEEP, blocks=(binding.PagesStruct * 2)(pages(), pages(**kw))), {}) == EINVAL
 
 
 def test_keep_wants_blocks_alike(lib):
