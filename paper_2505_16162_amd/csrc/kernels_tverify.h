@@ -18,9 +18,10 @@ namespace ks {
 // tv_stats_kernel: largest value and sum of exponentials of every 2048 values of every row, a wavefront each, so that any row spreads over the chip. It reads the logits
 // once; what bounds it are the exponentials: 17 instructions in 64 bits a value, and what a wavefront does besides (whose row it is, sums over its lanes). 284 rows of 152064 values in bf16:
 // 33.7 us, 2.6 TB/s (without the exponentials 20.7, without the loads 23.5).
+// tv_stats_table_kernel: the same of large batches in bf16, with a table of the powers in place of the polynomial.
 // tv_walk_kernel: a workgroup per request puts rows together, gets all drafted tokens' probabilities at once, walks, and picks the next token.
 // tv_sum_kernel: S behind a rejection, spread over the chip.
-// Walks take 9 us (one tree of 26 rows, 32000 tokens), a chain of dependent loads and steps.
+// Walks take 8 us (one tree of 26 rows, 32000 tokens), a chain of dependent loads and steps.
 // ------------------------------------------------------------------------------------------
 constexpr int TV_CHUNK = 2048;                                // values of a wavefront
 constexpr int TV_MAX_CHUNKS = KNNSSD_MAX_VOCAB / TV_CHUNK;
@@ -245,29 +246,42 @@ __device__ __forceinline__ TvBits tv_bits(const TvRaw<bf16_t> *raw) {
     return TvBits{max(top[0], top[1]) << 16, (unsigned int)max(low[0], low[1]) << 16};
 }
 
+// The table of powers 2^(v k) in LDS: entry 2 x + (v < 0) for the x-th |v| from 2^-17 on, x = 1 .. TT_LAST - 1. What is smaller finds NaN (and 0 does), also what is larger and powers beyond
+// 2^1000; -inf, and what is below -2^8 or 2^-1000, counts as nothing.
+constexpr int TT_LOW = (127 - 17) << 7, TT_LAST = ((127 + 8) << 7) - TT_LOW + 1;
+constexpr int TT_NT = 1024, TT_WGS = 256;                     // one workgroup to a compute unit (as two of 512 threads, with twice the tables to make: 57 us instead of 55)
+
+// sum of 2^((v - top) k) of a chunk's values; false: some are not in the table
+__device__ __forceinline__ bool tv_table_sum(const TvRaw<bf16_t> *raw, const double *table, TvBits bits, float top, double k, double *out) {
+    const unsigned int base = (unsigned int)(uintptr_t)(const __attribute__((address_space(3))) double *)table;
+    double sum = 0.0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        double x[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned int two = raw[q].w[0][e];
+            const tv_ushorts size = __builtin_bit_cast(tv_ushorts, two & 0x7fff7fffu);
+            const tv_ushorts of = __builtin_elementwise_min(__builtin_elementwise_sub_sat(size, (tv_ushorts)(TT_LOW - 1)), (tv_ushorts)TT_LAST);
+            const unsigned int at = __builtin_bit_cast(unsigned int, (tv_ushorts)(of << 4)) | __builtin_bit_cast(unsigned int, (tv_ushorts)(__builtin_bit_cast(tv_ushorts, two) >> 12)) & 0x00080008u;
+            x[2 * e] = *(const __attribute__((address_space(3))) double *)(uintptr_t)(base + (at & 0xffffu));
+            x[2 * e + 1] = *(const __attribute__((address_space(3))) double *)(uintptr_t)(base + (at >> 16));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        sum += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    }
+    const double all = tv_lane(tv_upto(sum), 63), top_k = top * k;
+    // (nothing is left out but what is 2^-200 of the sum, at most)
+    if (!(all > 0.0 && top_k > -700.0) || (__any(bits.low >= 0xc3800000u) && !((top + 256.0) * k > 200.0))) return false;
+    *out = all * tv_exp2(-top_k);
+    return true;
+}
+
 // Exponentials of a chunk are taken as 2^(v k - E), E the whole number next to top k: what v k is beyond a whole number has nothing to do with the top, and E goes to the exponent.
 // So a value costs 17 instructions, eight of them the polynomial's.
-template <typename T>
-__global__ __launch_bounds__(256) void tv_stats_kernel(TvArgs a) {
-    const int lane = threadIdx.x & 63;
-    int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    const bool draft = unit >= a.n_rows * a.chunks;
-    if (draft) unit -= a.n_rows * a.chunks;
-    const int row = unit / a.chunks, chunk = unit - row * a.chunks;
-    if (row >= a.n_rows || (draft && !a.draft)) return;       // (from here on wavefronts are on their own)
-    const int r = battn_request(a.row_start, a.n_requests, row);
-    const RowsRange rows = rows_of(a.row_start, r, a.n_rows);
-    const int i = row - rows.first;
-    if (i < 0 || i >= rows.n || i >= KNNSSD_MAX_TREE) return;
-    if (draft) {                                              // a row without children: its draft's logits are nobody's
-        bool child = false;
-        for (int j = i + 1 + lane; j < min(rows.n, KNNSSD_MAX_TREE); j += 64) child = child || a.parents[rows.first + j] == i;
-        if (!__any(child)) return;
-    }
-    const T *from = (const T *)(draft ? a.draft : a.logits) + row * (draft ? a.draft_stride : a.logits_stride);
-    TvRaw<T> raw[4];
-    tv_load<T, 4>(from, chunk, 0, lane, a.vocab, raw);
-    const float t = a.temperature[r];
+// TABLE (bf16): from the powers of all values in range, where all of the chunk's are.
+template <typename T, bool TABLE>
+__device__ __forceinline__ TvStat tv_stat(const TvArgs &a, const T *from, int chunk, int lane, float t, const TvRaw<T> *raw, const double *table) {
     const double k = 1.4426950408889634 / (double)t;
     // fp32 bits as signed numbers: the largest is the largest value, if that is not negative, and +inf or more where there is one or a NaN; as unsigned numbers: more than -inf where there is a negative NaN
     const TvBits bits = tv_bits(raw);
@@ -287,6 +301,10 @@ __global__ __launch_bounds__(256) void tv_stats_kernel(TvArgs a) {
     double sum = 0.0;
     int first = INT32_MAX;
     if (t > 0.f && top > -INFINITY && !bad) {
+        if constexpr (TABLE) {
+            if (t <= FLT_MAX && tv_table_sum(raw, table, bits, top, k, &sum)) return TvStat{top, first, sum};
+            sum = 0.0;
+        }
         // Against the lane's own largest value: nothing waits for the wavefront's. (One that has none takes the wavefront's, and what it sums up is nothing.)
         const float mine = own > -INFINITY ? own : top, least = tv_least(mine, t);
         const double mk = mine * k, top_k = top * k;
@@ -345,7 +363,108 @@ __global__ __launch_bounds__(256) void tv_stats_kernel(TvArgs a) {
         }
         first = tv_min(first);
     }
-    if (lane == 0) a.stats[(size_t)(draft ? a.n_rows : 0) * a.chunks + unit] = TvStat{bad ? 0.f : top, first, bad ? (double)NAN : sum};
+    return TvStat{bad ? 0.f : top, first, bad ? (double)NAN : sum};
+}
+
+// whether row i of a request has children: if not, its draft's logits are nobody's
+__device__ __forceinline__ bool tv_has_children(const TvArgs &a, RowsRange rows, int i, int lane) {
+    bool child = false;
+    for (int j = i + 1 + lane; j < min(rows.n, KNNSSD_MAX_TREE); j += 64) child = child || a.parents[rows.first + j] == i;
+    return __any(child);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void tv_stats_kernel(TvArgs a) {
+    const int lane = threadIdx.x & 63;
+    int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const bool draft = unit >= a.n_rows * a.chunks;
+    if (draft) unit -= a.n_rows * a.chunks;
+    const int row = unit / a.chunks, chunk = unit - row * a.chunks;
+    if (row >= a.n_rows || (draft && !a.draft)) return;       // (from here on wavefronts are on their own)
+    const int r = battn_request(a.row_start, a.n_requests, row);
+    const RowsRange rows = rows_of(a.row_start, r, a.n_rows);
+    const int i = row - rows.first;
+    if (i < 0 || i >= rows.n || i >= KNNSSD_MAX_TREE) return;
+    if (draft && !tv_has_children(a, rows, i, lane)) return;
+    const T *from = (const T *)(draft ? a.draft : a.logits) + row * (draft ? a.draft_stride : a.logits_stride);
+    TvRaw<T> raw[4];
+    tv_load<T, 4>(from, chunk, 0, lane, a.vocab, raw);
+    const TvStat stat = tv_stat<T, false>(a, from, chunk, lane, a.temperature[r], raw, nullptr);
+    if (lane == 0) a.stats[(size_t)(draft ? a.n_rows : 0) * a.chunks + unit] = stat;
+}
+
+// The same of large batches in bf16, with 2^(v k) for all bf16 values of 2^-17 <= |v| < 2^8 in LDS: a value is then seven instructions and a read, its sum against nothing, as such powers
+// have room in 64 bits. A workgroup has a run of chunks, a request's behind another's, and makes the table anew where the temperature changes. Of a request's chunks the first
+// sixteen of all its rows come first, then the next ones, so that draft's rows that nobody looks at (no children) are no run's alone.
+__global__ __launch_bounds__(TT_NT, 4) void tv_stats_table_kernel(TvArgs a) {
+    __shared__ double table[2 * TT_LAST + 2];
+    __shared__ int inner[KNNSSD_MAX_TREE];                    // 1 + the last request whose row of this number has children
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool drawn = a.draft != nullptr;
+    const int sides = drawn ? 2 : 1;
+    const long long units = (long long)max(0, min(a.n_rows, a.row_start[a.n_requests])) * sides * a.chunks;
+    const int begin = (int)(units * blockIdx.x / gridDim.x), end = (int)(units * (blockIdx.x + 1) / gridDim.x);
+    for (int i = tid; i < KNNSSD_MAX_TREE; i += TT_NT) inner[i] = 0;
+    float table_t = 0.f;
+    for (int at = begin, next; at < end; at = next) {
+        const int row0 = at / (sides * a.chunks), r = battn_request(a.row_start, a.n_requests, row0);
+        const RowsRange rows = rows_of(a.row_start, r, a.n_rows);
+        const int first = rows.first, n = rows.n, per = sides * n;
+        const bool inside = row0 >= first && row0 < first + n;
+        next = min(end, (inside ? first + n : row0 + 1) * sides * a.chunks);
+        if (!inside) continue;
+        const int x0 = at - first * sides * a.chunks + wave, x1 = next - first * sides * a.chunks;
+        const float t = a.temperature[r];
+        auto place = [&](int x, int *j, int *chunk) __attribute__((always_inline)) {
+            constexpr int W = TT_NT / 64;
+            const int turn = x / (per * W), in = x - turn * per * W, width = min(W, a.chunks - turn * W);
+            *j = in / width;
+            *chunk = turn * W + in - *j * width;
+        };
+        // a unit's values on their way; false: nobody looks at them
+        auto load = [&](int x, bool known, TvRaw<bf16_t> *raw) __attribute__((always_inline)) {
+            if (x >= x1) return false;
+            int j, chunk;
+            place(x, &j, &chunk);
+            const int i = j < n ? j : j - n;
+            if (i >= KNNSSD_MAX_TREE || (known && j >= n && __builtin_amdgcn_readfirstlane(inner[i]) != r + 1)) return false;
+            tv_load<bf16_t, 4>(j < n ? (const bf16_t *)a.logits + (first + i) * a.logits_stride : (const bf16_t *)a.draft + (first + i) * a.draft_stride, chunk, 0, lane, a.vocab, raw);
+            return true;
+        };
+        TvRaw<bf16_t> raw[4], ahead[4];
+        bool here = load(x0, false, raw);
+        __syncthreads();
+        if (drawn)
+            for (int j = 1 + tid; j < min(n, KNNSSD_MAX_TREE); j += TT_NT) {
+                const int p = a.parents[first + j];
+                if (p >= 0 && p < j) inner[p] = r + 1;
+            }
+        if (t > 0.f && t <= FLT_MAX && t != table_t) {
+            const double k = 1.4426950408889634 / (double)t;
+            for (int x = tid; x <= TT_LAST; x += TT_NT) {     // (0: smaller ones and 0; the last: larger ones, -inf)
+                const double vk = (double)__uint_as_float((unsigned int)(x + TT_LOW - 1) << 16) * k, y = tv_exp2(fmin(vk, 1000.0));
+                const bool beyond = x == TT_LAST || vk > 1000.0;
+                table[2 * x] = x == 0 || beyond ? (double)NAN : y;
+                table[2 * x + 1] = x == 0 ? (double)NAN : beyond ? 0.0 : 1.0 / y;
+            }
+            table_t = t;
+        }
+        __syncthreads();
+        for (int x = x0; x < x1; x += TT_NT / 64) {
+            const bool then = load(x + TT_NT / 64, true, ahead);
+            int j, chunk;
+            place(x, &j, &chunk);
+            const int i = j < n ? j : j - n;
+            if (here && (j < n || __builtin_amdgcn_readfirstlane(inner[i]) == r + 1)) {
+                const bf16_t *from = j < n ? (const bf16_t *)a.logits + (first + i) * a.logits_stride : (const bf16_t *)a.draft + (first + i) * a.draft_stride;
+                const TvStat stat = tv_stat<bf16_t, true>(a, from, chunk, lane, t, raw, table);
+                if (lane == 0) a.stats[((size_t)(j < n ? 0 : a.n_rows) + first + i) * a.chunks + chunk] = stat;
+            }
+            here = then;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) raw[q] = ahead[q];
+        }
+    }
 }
 
 // a row's chunks put together by a group of `width` lanes, four chunks a lane at a time

@@ -85,10 +85,17 @@ static bool values_ok(const void *base, int64_t stride, int32_t vocab, int32_t d
 //   chains of 1 to 9 rows, 8192 tokens 19, 25, 28, 31, 40; 32000 35, 29, 32, 35, 39; 152064 102, 42, 44, 47, 50
 static int verify_rounds(int chunks, int most_children) { return chunks <= 8 ? 0 : most_children == 1 ? 1 : chunks <= 24 ? 2 : 4; }
 
+// Whether the rows' sums are taken by a table of powers (bf16): where there are enough chunks for a table in every compute unit, and for each request's. Whole calls, us, without / with:
+//   256 requests of 4 rows of 50000 (25 600 chunks) 46 / 36; 16 of 24 of 152064 (28 800) 52 / 42; 256 of 1 of 152064 (19 200) 36 / 29; 1 of 120 of 152064 (9000) 34 / 33; 128 of 2 of 64000
+//   (8192, 64 a request) 24.2 / 24.1; 64 of 1 of 152064 (4800) 21.2 / 21.8; 512 of 1 of 32000 (8192, 16 a request) 23 / 26.5; drawn chains of 9 rows, 256 of 152064 535 / 365, 64 of 64000 74 / 68
+// Where it has nothing to give it costs: all greedy (16 of 24) 27 / 31; a logit of exactly 0 in every chunk 52 / 68.
+static bool by_table(const TvArgs &a, unsigned units) { return units >= 8192 && units / 64 >= (unsigned)a.n_requests; }
+
 template <typename T>
 static void launch_verify(const TvArgs &a, int rounds, hipStream_t s) {
     const unsigned units = (unsigned)a.n_rows * a.chunks * (a.draft ? 2 : 1);
-    hipLaunchKernelGGL((tv_stats_kernel<T>), dim3((units + 3) / 4), dim3(256), 0, s, a);
+    if (sizeof(T) == 2 && by_table(a, units)) hipLaunchKernelGGL(tv_stats_table_kernel, dim3(TT_WGS), dim3(TT_NT), 0, s, a);
+    else hipLaunchKernelGGL((tv_stats_kernel<T>), dim3((units + 3) / 4), dim3(256), 0, s, a);
     for (int i = 0; i <= rounds; ++i) {
         if (i > 0) hipLaunchKernelGGL((tv_sum_kernel<T>), dim3(a.chunks, a.n_requests), dim3(256), 0, s, a);
         hipLaunchKernelGGL((tv_walk_kernel<T>), dim3(a.n_requests), dim3(TV_NT), 0, s, a, i, i < rounds);
