@@ -504,7 +504,7 @@ def knnssd_tree_verify(logits: torch.Tensor, tokens: torch.Tensor, parents: torc
 
 
 class PageBlocks:
-    """The caches of a model's blocks (Pages of one shape, type and order), as knnssd_tree_keep takes them."""
+    """The caches of a model's blocks (Pages of one shape, type and order), as knnssd_tree_keep takes them: each once, also where blocks share one."""
 
     def __init__(self, blocks: Sequence[Pages]):
         self.blocks = list(blocks)
