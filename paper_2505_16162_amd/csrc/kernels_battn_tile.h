@@ -4,6 +4,7 @@
 #include <climits>
 
 #include "battn_common.h"
+#include "tile_deal.h"
 
 namespace ks {
 
@@ -19,7 +20,6 @@ namespace ks {
 // 51 % of the time, the vector unit as much; on zeros, where the power limit leaves more clock, a quarter faster); eight chunks of up to 900 rows over 700 to 9000 positions in pages, 40 heads over 8: 485 us = 783 TFLOP/s. In fp32 the matrix instructions
 // themselves: a sixteenth of the bf16 rate.
 // ------------------------------------------------------------------------------------------
-constexpr int BT_PAIRS = 128;
 // What a lane's weights of a block may add up to before their reference follows the scores. Sums of values times weights have that much less room: 2^33 times the blocks of an
 // axis, times the values, has to stay below 2^128. Following costs nothing where scores have a standard deviation of 1 or 4; of 8, prompts of 4096 rows take 366 us, as
 // with 2^64, with 2^24 374, with 2^16 391 (chunks 475, 489, 532).
@@ -56,32 +56,9 @@ __device__ __forceinline__ bool battn_find_tile(const BattnArgs &a, int index, i
 
 template <int HD, bool PAGED, int NP> constexpr int battn_tile_lds() { return 2 * 2 * battn_tile_positions<HD, PAGED, NP>() * HD * (NP == 0 ? 4 : 2); }
 
-// Over pages the batch's tiles are dealt to the workgroups in equal runs, as in battn_few_kernel, by their cost: a tile's is the positions before its request's
-// new rows times the heads of a group, and the pairs up to its own last one (a pair's rows counted exactly), or a block's cost, positions of a block times heads
-// of a group, if that is more. It is at most what its blocks hold, so a run that begins x into a tile begins with block
-// x / (a block's cost) of it, and a run of a block's cost or more is never empty. The costs before a tile have a closed form.
-struct TileShape {
-    int n, tiles, small;                // rows, tiles of a kv head, those of its first that cost a block
-    bool whole;                         // one cost for all of a kv head's tiles (`tiles` is 1): they are worked on side by side
-    long long step, pairs, block;       // cost of a tile without its own pairs; all pairs; a block's cost
-    __device__ __forceinline__ long long sloped(int t) const { return t * step + (long long)(BT_PAIRS / 2) * t * (t + 1); }
-    __device__ __forceinline__ long long before(int t) const { return t <= small ? t * block : small * block + sloped(t) - sloped(small); }      // (t < tiles)
-    __device__ __forceinline__ long long cost(int t) const { return max(block, step + (whole ? pairs : min((long long)(t + 1) * BT_PAIRS, pairs))); }
-    __device__ __forceinline__ long long total() const { return tiles ? before(tiles - 1) + cost(tiles - 1) : 0; }
-};
-constexpr int BT_FAR = 1 << 24;         // positions beyond count as so many
-__device__ __forceinline__ int battn_tiles(long long pairs) { return (int)((pairs + BT_PAIRS - 1) / BT_PAIRS); }
-__device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r, int positions, bool whole) {
-    TileShape f{0, 0, 0, whole, 0, 0, (long long)positions * a.group};
+__device__ __forceinline__ TileShape battn_tile_shape(const BattnArgs &a, int r, int positions, bool side_by_side) {
     const int n = rows_of(a.row_start, r, a.n_rows).n;
-    if (n > 0) {
-        f.n = n;
-        f.pairs = (long long)n * a.group;
-        f.tiles = whole ? 1 : battn_tiles(f.pairs);
-        f.step = (long long)min(max(battn_len(a, r) - n, 0), BT_FAR) * a.group;
-        f.small = (int)min((long long)f.tiles, max(f.block - f.step, 0ll) / BT_PAIRS);
-    }
-    return f;
+    return tile_shape(n, n > 0 ? battn_len(a, r) : 0, a.group, positions, side_by_side);
 }
 
 // NP: 1 all in bf16; 3 fp32 queries over a bf16 cache, which stay exact as three bf16 planes, as do the weights; 0 all in fp32, on the fp32 matrix
@@ -109,10 +86,8 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
     int run = 0;                                              // (its place among the runs that may hold parts of the same tiles)
     int slot_run = 0;                                         // its place in the workspace
     const long long block_cost = (long long)CH * a.group;
-    // Trees: the tiles of a kv head side by side, each in a workgroup of its own over the same positions, so that what one of them reads is in the die's L2 for the others. Then a
-    // run is a stretch of positions, and as many workgroups of one die share it as the batch's widest request has tiles.
-    bool whole = false;
-    int mine_of = 0, most_runs = (int)gridDim.x;              // this workgroup's tile; runs at most
+    bool side_by_side = false;                                // trees: a kv head's tiles are worked on at once
+    int mine_of = 0, most_runs = (int)gridDim.x;              // this workgroup's tile then; runs at most
     if constexpr (PAGED) {
         run = slot_run = battn_run();
         if constexpr (TREE) {
@@ -139,19 +114,13 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
             one = battn_same(one);
             all = battn_same(all);
             widest = battn_same(widest);
-            // (only where three quarters of those workgroups have a tile: two requests of 60 to 64 rows at 100 000 positions, three tiles, 393 -> 350 us; 24 requests of 8 to 64 rows,
-            // one to three tiles, 64 % of them, 86 -> 125)
-            whole = widest > 1 && widest <= 8 && all * 4 >= one * widest * 3;
-            if (whole) {
-                const int slots = gridDim.x >> 3, per = slots / widest, die = blockIdx.x & 7, slot = blockIdx.x >> 3;
-                most_runs = 8 * per;
-                mine_of = slot % widest;
-                run = die * per + slot / widest;
-                slot_run = mine_of * most_runs + run;
-                if (slot >= per * widest) {                   // (left over)
-                    slot_run = most_runs * widest + die * (slots - per * widest) + slot - per * widest;
-                    run = INT_MAX;
-                }
+            side_by_side = tiles_side_by_side(widest, one, all);
+            if (side_by_side) {
+                const TilePlace place = tile_place((int)blockIdx.x, (int)gridDim.x, widest);
+                run = place.run;
+                slot_run = place.slot_run;
+                most_runs = place.most_runs;
+                mine_of = place.mine_of;
             }
         }
         if (tid == 0) ((FewMerge *)a.ws)[slot_run] = FewMerge{0, 0, 0, 0, 0};
@@ -160,7 +129,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
             bool found = false;
             for (int q0 = 0; q0 < a.n_requests && !found; q0 += 64) {
                 long long upto = 0;
-                if (q0 + lane < a.n_requests) upto = battn_tile_shape(a, q0 + lane, CH, whole).total() * a.Hkv;
+                if (q0 + lane < a.n_requests) upto = battn_tile_shape(a, q0 + lane, CH, side_by_side).total() * a.Hkv;
                 for (int off = 1; off < 64; off <<= 1) {
                     const long long u = __shfl_up(upto, off);
                     if (lane >= off) upto += u;
@@ -189,7 +158,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
             }
             if (found) break;
         }
-        f = battn_tile_shape(a, r, CH, whole);
+        f = battn_tile_shape(a, r, CH, side_by_side);
         kvh = (int)battn_divide(at - before, f.total());
         before += kvh * f.total();
         int lo = 0, hi = f.tiles;
@@ -260,7 +229,7 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
         len = PAGED ? battn_same(battn_len(a, r)) : n;
         last = len - 1;
         base = len - n;                                       // position of the request's first new row
-        const int tile_last = battn_same((int)(((whole ? f.pairs : min((long long)(tile + 1) * BT_PAIRS, f.pairs)) - 1) / a.group));
+        const int tile_last = battn_same((int)((f.upto(tile) - 1) / a.group));
         n_blocks = (max(base, 0) + tile_last) / CH + 1;
         b0 = 0;
         b1 = n_blocks;
@@ -286,30 +255,15 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
     };
     // on to the next tile; false behind the run's last
     auto advance = [&]() __attribute__((always_inline)) {
-        before = battn_same(before + f.cost(tile));
-        bool goes_on = before < end;
-        if (goes_on) {
-            at = before;
-            if (++tile == f.tiles) {
-                tile = 0;
-                if (++kvh == a.Hkv) {
-                    kvh = 0;
-                    do {
-                        if (++r >= a.n_requests) goes_on = false;     // (never: the run lies in some requests)
-                        else f = battn_tile_shape(a, r, CH, whole);
-                    } while (goes_on && f.tiles == 0);
-                }
-            }
-        }
-        return goes_on;
+        return tile_advance(f, r, kvh, tile, before, at, end, a.Hkv, a.n_requests, mine_of,
+                            [&](int q) __attribute__((always_inline)) { return battn_tile_shape(a, q, CH, side_by_side); },
+                            [](long long v) __attribute__((always_inline)) { return battn_same(v); });
     };
-    if constexpr (TREE) {
-        while (whole && mine_of >= battn_tiles(f.pairs))      // the request has no such tile
-            if (!advance()) return;
-    }
+    if constexpr (TREE)
+        if (side_by_side && mine_of >= battn_tiles(f.pairs) && !advance()) return;         // the request has no such tile
     enter();
     while (b0 < b1) {
-        const long long p0 = (long long)(whole ? mine_of : tile) * BT_PAIRS;
+        const long long p0 = (long long)(side_by_side ? mine_of : tile) * BT_PAIRS;
         const int wave_first = battn_same((int)((p0 + wave * 32) / a.group));                                     // the wavefront's first row
         const int wave_last = battn_same(p0 + wave * 32 < f.pairs ? (int)((min(p0 + wave * 32 + 32, f.pairs) - 1) / a.group) : INT_MIN / 2);      // ... and last one
         const long long pair = min(p0 + wave * 32 + col, f.pairs - 1);
@@ -491,8 +445,6 @@ __global__ __launch_bounds__(256, HD == 128 && !PAGED && NP == 1 ? 3 : 2) void b
         // on to the next tile: its first block is on its way while this one is written (the buffer that it goes to has been read by all)
         if constexpr (PAGED) {
             goes_on = advance();
-            if constexpr (TREE)
-                while (goes_on && whole && mine_of >= battn_tiles(f.pairs)) goes_on = advance();
             if (goes_on) enter();
         }
         if (!live) {
