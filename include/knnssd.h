@@ -429,7 +429,8 @@ int32_t knnssd_tree_attention(const knnssd_pages *pages, const int32_t *block_ta
  *   draft_logits_dev NULL, the drafts were not drawn: child x is taken if p(x) > u S, else S loses p(x) and p(x) becomes 0
  * Where no child is taken the walk ends, and the next token is the first that the sum of max(p - c q, 0) (or of what is left of p) up to and with it is more than u_next[r] times the whole sum. So a
  * request of a single row draws a token from its logits. A request's path_dev[row_start[r] + j], j < n_path[r], are its rows taken, row 0 first, -1 behind; next_token_dev[r] comes
- * behind them. All sums are in 64 bits. Numbers from [0, 1) belong in u_accept_dev and u_next_dev.
+ * behind them. All sums are in 64 bits, of exponentials that are off by up to 2.2e-12 of them; in the sums of max(p - c q, 0) and where the next token is picked, values of p (and of q) that are 2^-500 of their row's
+ * largest and less count as nothing, so that such a token is not the next one under a u_next of 0 either. Numbers from [0, 1) belong in u_accept_dev and u_next_dev.
  * next_token[r] is -1 where there is no distribution to go by: a request without rows or with a temperature that is negative or not finite (n_path is 0 then), a row on the path whose logits (or, if it has
  * children, draft's logits) hold NaN or +inf or nothing but -inf, or nothing left of p. A drafted token outside the vocabulary is never taken; rows from
  * KNNSSD_MAX_TREE on of a request are none of the tree. most_children: an upper bound of a row's children if the caller has one, else 0; it only chooses the kernels.

@@ -794,7 +794,8 @@ __global__ __launch_bounds__(TV_NT) void tv_walk_kernel(TvArgs a, int round, int
                     summed ? 1.0 / p_row[node].sum : 1.0, summed ? c / q_row[node].sum : 0.0, k};
     if (!summed) {
         const TvStat *own = p_stats + (size_t)node * a.chunks;
-        for (int x = tid; x < a.chunks; x += TV_NT) chunk_sum[x] = own[x].top > -INFINITY ? own[x].sum * tv_exp2(((double)own[x].top - w.p_top) * k) : 0.0;
+        // (a chunk all of whose tokens are below the least has no weight, as it has none where a token is picked: under a target of 0 it would be the first one)
+        for (int x = tid; x < a.chunks; x += TV_NT) chunk_sum[x] = own[x].top >= w.p_least ? own[x].sum * tv_exp2(((double)own[x].top - w.p_top) * k) : 0.0;
         if (!drawn && inner[node])
             for (int i = tid; i < n; i += TV_NT)
                 if (parent[i] == node) rejected[atomicAdd(&now.n_rejected, 1)] = token[i];       // (in any order: all of them get a weight of 0)
