@@ -659,6 +659,7 @@ __global__ __launch_bounds__(TV_NT) void tv_walk_kernel(TvArgs a, int round, int
         if (wave == 0) {
             double left = 1.0;                                // what of p is left
             bool waits = false, lost = false;                 // for the sum over a row; at a row without a distribution
+            bool first = c == 0.0;                            // nothing has been rejected at the node (what is left may still be 1 behind a token of less than 2^-53)
             if (summed) {
                 left = 0.0;
                 for (int x = lane; x < a.chunks; x += 64) left += chunk_sum[x];
@@ -694,15 +695,14 @@ __global__ __launch_bounds__(TV_NT) void tv_walk_kernel(TvArgs a, int round, int
                     continue;
                 }
                 const int l = __builtin_ctzll(match), child = seg * 64 + l;
-                const bool untried = c == 0.0 && left == 1.0;
                 last = child;
                 bool take = taken >> l & 1;
                 double px = 0.0, qx = 1.0;
-                if (!untried || !take) {
+                if (!first || !take) {
                     const double u = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u_of), l));
                     px = tv_lane(p_of, l);
                     qx = tv_lane(q_of, l);
-                    if (!drawn && !untried) {                 // the same token again: it has been rejected
+                    if (!drawn && !first) {                   // the same token again: it has been rejected
                         const int x = __builtin_amdgcn_readlane(tok, l);
                         if (__any(par == node && tok == x && lane < l)) px = 0.0;
                         for (int i = (node & ~63) + lane; i < seg * 64; i += 64)
@@ -716,13 +716,16 @@ __global__ __launch_bounds__(TV_NT) void tv_walk_kernel(TvArgs a, int round, int
                     ++kept;
                     c = 0.0;
                     left = 1.0;
+                    first = true;
                     summed = false;
                     goes_on = with_children >> l & 1;
                     lost = without_one >> l & 1;
                 } else if (!drawn) {
                     left -= px;
+                    first = false;
                 } else if (qx > 0.0) {                        // (a token that the draft cannot have drawn says nothing about its distribution)
                     c += left;
+                    first = false;
                     waits = !greedy;
                     left = 1.0;                               // (greedy: p and q are each all on one token, not the same: p stays)
                 }

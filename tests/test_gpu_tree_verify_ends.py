@@ -53,3 +53,18 @@ def test_a_number_of_0_where_the_first_tokens_are_next_to_impossible(dtype, temp
     assert outcome(x, [0, 2060], [-1, 0], [0.0, 0.9999], temperature, 0.0, rows=rows) == ([0], 2067 if first else 0)
     outcome(x, [0, few], [-1, 0], [0.0, 0.9999], temperature, 0.0, q, rows=rows)
     assert outcome(x, [0, top], [-1, 0], [0.0, 0.0], temperature, 0.0, q, rows=rows) == ([0, 1], first)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("again", [2, 63, 64, 70, 200])
+def test_a_token_of_next_to_no_probability_again_with_a_number_of_0(dtype, again):
+    """A given draft of 10^-26 is tried once and rejected; what is left of p has nothing on its token, so no number takes it, not even 0, though the rest still sums up to 1 in 64 bits."""
+    n = again + 2
+    x = torch.tensor([[0.0, 60.0, 59.0, -math.inf]] * n).to(dtype)
+    tokens, parents, u = [3] * n, [0] * n, [0.5] * n
+    parents[0] = -1
+    tokens[1] = tokens[again] = 0
+    u[again] = 0.0
+    tokens[again + 1] = 1
+    assert outcome(x, tokens, parents, u, 1.0, 0.5) == ([0, again + 1], 1)
+    assert outcome(x, tokens[:-1], parents[:-1], u[:-1], 1.0, 0.0) == ([0], 1)
