@@ -2,6 +2,7 @@
 #pragma once
 #include <cfloat>
 
+#include "batch_route.h"
 #include "battn_common.h"
 
 namespace ks {
@@ -18,8 +19,7 @@ namespace ks {
 // 12 requests of 2 to 5 rows, 40 kv heads of 128, fp32 queries: 413 MB in 84 us with the merge, 4.9 TB/s.
 // ------------------------------------------------------------------------------------------
 
-// positions of a unit: 8 KB of keys, 8 KB of values, which a wavefront holds in registers
-template <int HD> __host__ __device__ constexpr int battn_few_positions() { return 32 * 128 / HD; }
+template <int HD> __host__ __device__ constexpr int battn_few_positions() { return few_positions(HD); }
 // units of request r: rows, blocks of a group, groups of pairs per kv head
 struct FewShape { int n, blocks, pair_groups; };
 __device__ __forceinline__ FewShape battn_few_shape(const BattnArgs &a, int r, int group_pairs, int positions) {

@@ -3,6 +3,7 @@
 
 #include <cmath>
 
+#include "batch_route.h"
 #include "hip_try.h"
 #include "kernels_battn_few.h"
 #include "kernels_battn_row.h"
@@ -108,31 +109,9 @@ static void launch_prompt_tiles(const BattnArgs &a, hipStream_t s) {
     hipLaunchKernelGGL((battn_tile_kernel<HD, false, NP, false>), dim3((unsigned)tiles_bound(a)), dim3(256), (battn_tile_lds<HD, false, NP>()), s, a);
 }
 
-// Most (row, head) pairs of one kv head that a request may have for battn_few_kernel to take the batch: as many as one group holds; each further group reads the cache
-// again. Whole calls, us, few rows / tiles, 32 requests at 200 to 4000 positions, bf16 queries; fp32 ones (whose tiles do three times the products):
-//   40 heads of 128 over 8: 5 pairs 62 / 68; 59 / 83, 10 to 15 64 / 72; 67 / 91, 20 77 / 57; 104 / 88, 20 to 30 92 / 63; 85 / 78, 35 to 60 133 / 64; 189 / 118
-//   40 over 40: 1 pair 233 / 271; 240 / 296, 16 293 / 306; 286 / 339, 20 527 / 319; 557 / 404, 60 972 / 384; 1011 / 433
-//   32 heads of 64 over 8: 8 to 12 29 / 31; 34 / 52, 16 34 / 39; 40 / 54, 16 to 24 42 / 38; 51 / 57, 28 to 48 58 / 37; 70 / 64
-// Two requests of 20 to 30 pairs at 100 000 positions 223 / 157; 227 / 167. The bound is the caller's most_rows, or all rows of the batch.
-static const int FEW_PAIRS = 16;
-
-// what battn_few_kernel has to do, at most: blocks of positions for every group of pairs
-template <int HD> static int64_t few_units(const BattnArgs &a, int64_t groups) {
-    const int ch = battn_few_positions<HD>();
-    const int64_t blocks = (((int64_t)a.width << a.shift) + ch - 1) / ch;
-    return blocks < INT32_MAX ? blocks * groups * a.Hkv : INT64_MAX;
-}
-static int64_t few_groups(const BattnArgs &a) { return ((int64_t)a.n_rows * a.group + FEW_PAIRS - 1) / FEW_PAIRS + a.n_requests; }
-
-// Trees have many pairs from the start, but few trees over short contexts are done before a tile's first block is: whole calls, us, battn_few_kernel / tiles, one request, 40 heads of 128 over 8, bf16:
-//   26 rows over 400 positions 16 / 25, 1500 21 / 24, 3000 (7600 units) 24 / 27, 6000 (15 000) 30 / 29; 60 rows 400 16 / 26, 1500 (8400) 23 / 28, 3000 (16 000) 31 / 31, 6000 44 / 33
-//   40 heads over 40: 60 rows over 1500 (9900) 24 / 28; four requests of 26 rows over 1500 (15 000) 30 / 29
-// The positions are those that the table can hold.
-static const int64_t FEW_UNITS = 12288;
-
 template <int HD, int NP, bool TREE>
 static void launch_few(const BattnArgs &a, int64_t most, hipStream_t s) {
-    const int64_t groups = few_groups(a), units = few_units<HD>(a, groups);      // at most
+    const int64_t groups = few_groups(a.n_rows, a.group, a.n_requests), units = few_units((int64_t)a.width << a.shift, HD, groups, a.Hkv);      // at most
     const unsigned runs = (unsigned)(units / 4 + 1 < BF_WGS ? (units / 4 + 8) & -8 : BF_WGS);
     hipLaunchKernelGGL((battn_few_kernel<HD, NP, TREE>), dim3(runs), dim3(256), 0, s, a);
     launch_merge<HD, NP>(a, runs, (int)(most < FEW_PAIRS ? most : FEW_PAIRS), groups * a.Hkv, FEW_PAIRS, s);
@@ -150,7 +129,7 @@ static void launch_paged(const BattnArgs &a, int32_t dtype, int32_t kv_dtype, in
     if (kv_dtype == KNNSSD_FP32) {
         if (rows_alone(a, (int64_t)a.width << a.shift)) hipLaunchKernelGGL((battn_row_kernel<HD, true, TREE>), dim3((unsigned)(a.n_rows * a.H)), dim3(256), 0, s, a);
         else launch_paged_tiles<HD, 0, TREE>(a, most, s);
-    } else if (most <= FEW_PAIRS || (TREE && few_units<HD>(a, few_groups(a)) <= FEW_UNITS)) {
+    } else if (goes_to_few(TREE, (int64_t)a.width << a.shift, HD, a.n_rows, a.group, a.n_requests, a.Hkv, most)) {
         if (dtype == KNNSSD_FP32) launch_few<HD, 3, TREE>(a, most, s);
         else launch_few<HD, 1, TREE>(a, most, s);
     } else {
