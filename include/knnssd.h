@@ -432,7 +432,8 @@ int32_t knnssd_tree_attention(const knnssd_pages *pages, const int32_t *block_ta
  * behind them. All sums are in 64 bits, of exponentials that are off by up to 2.2e-12 of them; in the sums of max(p - c q, 0) and where the next token is picked, values of p (and of q) that are 2^-500 of their row's
  * largest and less count as nothing, so that such a token is not the next one under a u_next of 0 either. Numbers from [0, 1) belong in u_accept_dev and u_next_dev.
  * next_token[r] is -1 where there is no distribution to go by: a request without rows or with a temperature that is negative or not finite (n_path is 0 then), a row on the path whose logits (or, if it has
- * children, draft's logits) hold NaN or +inf or nothing but -inf, or nothing left of p. A drafted token outside the vocabulary is never taken; rows from
+ * children, draft's logits) hold NaN or +inf or nothing but -inf, or nothing left of p (S of given drafts is
+ * 1 less what was tried, in 64 bits: where they are all of p's tokens and all but 10^-12 of it has been rejected, the last one may be too). A drafted token outside the vocabulary is never taken; rows from
  * KNNSSD_MAX_TREE on of a request are none of the tree. most_children: an upper bound of a row's children if the caller has one, else 0; it only chooses the kernels.
  * ws_dev: knnssd_tree_verify_bytes (drawn: draft_logits_dev is given; 0: sizes that the call refuses), 256-byte aligned, of any contents; nothing in it outlives a call. The same call gives the same result.
  * KNNSSD_ESHAPE for vocab outside [1, KNNSSD_MAX_VOCAB], KNNSSD_ERANGE for n_requests outside [1, KNNSSD_MAX_REQUESTS], n_rows outside [1, KNNSSD_MAX_ROW_HEADS / 4] or
