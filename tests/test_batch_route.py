@@ -61,5 +61,5 @@ def test_the_cases_for_the_tiles_go_there(route):
 
 def test_few_trees_over_short_contexts_do_not(route):
     c = dict(rows=[26], lens=[1500], heads=40, kv_heads=8, dim=128)
-    assert route(c, 1536, 64)[0] and route(c, 3072 + 64, 64)[0] and not route(c, 6144, 64)[0]
+    assert route(c, 1536, 64)[0] and route(c, 4032, 64)[0] and not route(c, 6016, 64)[0]
     assert route(dict(c, rows=[3], most=True), 1 << 30, 64)[0]
